@@ -85,6 +85,7 @@ enum { DG_MMA_16X16X32_BF16 = 1, /* group of 32 */
 enum { DG_CARRY = 0, DG_SEQ = 1, DG_TREE = 2 };  /* combine rules */
 enum { DG_TAIL_LAST = 0, DG_TAIL_FIRST = 1 };     /* short K tile position (k_loop_step) */
 enum { DG_F32 = 0, DG_BF16 = 1 };                  /* storage/rounding types */
+enum { DG_F16 = 2, DG_E4M3 = 3 };                  /* more of them, where an operator names them */
 enum { DG_EPI_NONE = 0, DG_EPI_BIAS = 1, DG_EPI_BIAS_SILU = 2 };
 enum { DG_ROUND_FINAL = 0, DG_ROUND_PRE_ACT = 1 };
 enum { DG_OP_SUM = 0, DG_OP_SUMSQ = 1 };
@@ -499,6 +500,7 @@ dg_status dg_softmax(const dg_desc* d, const float* X, void* Y, int64_t rows, in
  * above the diagonal are masked.  So q_block (BLOCK_M) takes part in a
  * causal answer whenever it is not a multiple of key_block. */
 enum { DG_ATTN_DIV = 0, DG_ATTN_RECIP = 1 };
+enum { DG_EXP2_LIB = 0, DG_EXP2_INST = 1 };        /* attention's exponential */
 
 typedef struct {
   uint32_t struct_size;   /* sizeof(dg_attn_params) */
@@ -510,7 +512,11 @@ typedef struct {
   int32_t pv_fma;         /* 1: the rescaled output row is the P.V accumulator */
   int32_t l_fma;          /* 1: the denominator update is one fused multiply-add */
   int32_t final_div;      /* DG_ATTN_DIV: O / l;  DG_ATTN_RECIP: O * (1 / l) */
-  int32_t out_dtype;      /* DG_F32 or DG_BF16 */
+  int32_t out_dtype;      /* DG_F32 or DG_BF16 (DG_F16 too over a paged cache) */
+  /* The fields below belong to dg_attention_paged (dg_attention takes 0, 0; a
+   * struct_size that ends before them means 0, 0). */
+  int32_t split_keys;     /* keys per span, a multiple of key_block; 0: one span */
+  int32_t exp2;           /* DG_EXP2_LIB: as above;  DG_EXP2_INST: the part's exponential */
 } dg_attn_params;
 
 typedef struct dg_attn_desc dg_attn_desc; /* opaque, immutable */
@@ -537,6 +543,143 @@ void dg_attn_desc_destroy(dg_attn_desc* d);
 dg_status dg_attention(const dg_attn_desc* d, const void* Q, const void* K, const void* V, void* O,
                        int64_t H, int64_t Lq, int64_t Lk, int64_t dim, float qk_scale, void* stream);
 
+/* ---------------------------------------------- positions and a paged cache
+ *
+ * Rotary positions.  Of every head the first `rotary` of dim elements are
+ * rotary / 2 pairs: pair i is (x_i, x_{i + rotary / 2}) (DG_ROPE_HALF) or
+ * (x_2i, x_{2i + 1}) (DG_ROPE_ADJACENT).  It turns by the angle whose cosine c
+ * and sine s are column i of row pos[pair_axis[i]][t] of the two tables:
+ *   y1 = RN32(RN32(x1 c) - RN32(x2 s)),  y2 = RN32(RN32(x2 c) + RN32(x1 s)),
+ * rounded once to the output's type; the other elements are copied.  Several
+ * axes (time, height, width, ...) each have a row of pos.  A position outside
+ * the tables turns its pairs into NaN. */
+enum { DG_ROPE_HALF = 0, DG_ROPE_ADJACENT = 1 };
+#define DG_ROPE_MAX_DIM 512
+#define DG_ROPE_MAX_AXES 4
+
+typedef struct {
+  uint32_t struct_size;      /* sizeof(dg_rope_params) */
+  int32_t dim;               /* elements per head, even, 2..DG_ROPE_MAX_DIM */
+  int32_t rotary;            /* elements that turn, even, 2..dim */
+  int32_t pairing;           /* DG_ROPE_HALF or DG_ROPE_ADJACENT */
+  int32_t n_axes;            /* 1..DG_ROPE_MAX_AXES */
+  const uint8_t* pair_axis;  /* host array, the axis of each of rotary / 2 pairs (copied at
+                                create time); NULL: axis 0 (n_axes must be 1) */
+} dg_rope_params;
+
+typedef struct dg_rope_desc dg_rope_desc; /* opaque, immutable */
+
+/* Validate p and build a rotation (free with dg_rope_desc_destroy).
+ * DG_ERR_INVALID for NULL arguments, a small struct_size or a field out of range. */
+dg_status dg_rope_desc_create(const dg_rope_params* p, dg_rope_desc** out);
+void dg_rope_desc_destroy(dg_rope_desc* d);
+
+/* Y = X turned by its tokens' positions; inverse = 1 turns back (s replaced by
+ * -s), which is also the gradient: dX from dY.
+ *   X, Y: device, T tokens x H heads x dim of dtype (DG_F32, DG_BF16 or
+ *   DG_F16), element (t, h, e) at t * token + h * head + e in elements.  Y
+ *   may be X itself with the same strides; otherwise they may not overlap, and
+ *   Y's rows may not overlap each other.
+ *   pos: device, n_axes x T int32;  cos_t, sin_t: device, table_rows x
+ *   rotary / 2 fp32.
+ * T = 0 or H = 0 is a no-op.  DG_ERR_SHAPE for negative sizes or strides or T
+ * over 2^31 - 1, DG_ERR_INVALID for overlapping rows or a NULL pointer,
+ * DG_ERR_ALIGN for a pointer not aligned to its element.  One launch; rows and
+ * strides of whole 16-byte pieces are faster. */
+dg_status dg_rope(const dg_rope_desc* d, int32_t dtype, const void* X, int64_t x_token, int64_t x_head,
+                  void* Y, int64_t y_token, int64_t y_head, const int32_t* pos, const float* cos_t,
+                  const float* sin_t, int64_t table_rows, int64_t T, int64_t H, int32_t inverse, void* stream);
+
+/* A paged cache of keys and values: `pages` pages of `page` tokens of `heads`
+ * heads of dim elements of dtype, K and V laid out alike: element (p, t, h, e)
+ * at p * page_stride + t * token_stride + h * head_stride + e in elements, so
+ * [pages][page][heads][dim] and [pages][heads][page][dim] are both fine.
+ * DG_E4M3 elements stand for their value times k_scale (v_scale); the other
+ * types take scales of 1.  Token t of a page is slot p * page + t. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(dg_kv_cache) */
+  int32_t dtype;             /* DG_BF16, DG_F16 or DG_E4M3 */
+  void* K;                   /* device, 16-byte aligned, like V */
+  void* V;
+  int64_t pages, page, heads, dim;
+  int64_t page_stride, token_stride, head_stride;   /* whole 16-byte pieces */
+  float k_scale, v_scale;    /* finite and above 0 */
+} dg_kv_cache;
+
+/* Appends T tokens to the cache: token t's keys, turned by r, and its values go
+ * to slot slots[t]; a slot below 0 or past the cache's last is left out (the
+ * rows of a padded batch).  Elements are rounded once, from binary32, to the
+ * cache's type: e4m3 as RN(x / scale) cut to +-448.  With Q, its heads are
+ * turned the same way into Qout (every token's, slot or not).
+ *   in_dtype: DG_BF16 or DG_F16, the cache's type, or DG_BF16 over e4m3.
+ *   Q, Qout: T x q_heads x dim (both NULL: keys and values only), overlapping
+ *   as dg_rope's X and Y may;  K, V: T x heads x dim, not part of the cache or of
+ *   Qout; strides in elements.
+ *   r NULL: nothing turns (Q must be NULL; pos and the tables are not read).
+ * Two tokens with one slot leave one of them there, or parts of both: give
+ * every token a slot of its own.  T = 0 is a no-op.  One launch.  Errors as
+ * dg_rope, DG_ERR_UNSUPPORTED for a pair of types that is not listed,
+ * DG_ERR_SHAPE for a rotation of another dim than the cache's. */
+dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_dtype, const void* Q,
+                       int64_t q_token, int64_t q_head, void* Qout, int64_t qo_token, int64_t qo_head,
+                       int64_t q_heads, const void* K, int64_t k_token, int64_t k_head, const void* V,
+                       int64_t v_token, int64_t v_head, const int32_t* pos, const float* cos_t,
+                       const float* sin_t, int64_t table_rows, const int64_t* slots, int64_t T, void* stream);
+
+/* Attention of a ragged batch over the cache.  Sequence b has the new tokens
+ * cu_q[b] .. cu_q[b + 1] - 1 of Q and kv_len[b] keys, token t of them in page
+ * page_table[b][t / page]; with a causal descriptor its new tokens are the last
+ * of the kv_len[b] (new token j of n sees the keys 0 .. kv_len[b] - n + j), with
+ * an unmasked one each sees all of them.  Query head h reads key head
+ * h / (q_heads / heads).  Per row the order is the descriptor's: key blocks of
+ * key_block from key 0 as above, but that a key which the row does not see
+ * drops out (p = 0) instead of getting -1e6, in spans of split_keys keys.
+ * Each span starts anew from m = -inf, l = +0, O = +0; span 0's state is the
+ * row's (M, L, T), and each later span that the row sees joins it in turn:
+ *   mn = max(M, m);  a = exp2(M - mn);  b = exp2(m - mn);
+ *   L = fma(b, l, RN32(a L));  T = fma(b, O, RN32(a T));  M = mn.
+ * The answer is RN32(T / L or T * RN32(1 / L)) times v_scale, rounded to
+ * out_dtype; scores are scaled by RN32(qk_scale * k_scale).  While the maximum
+ * is -inf, 0 is subtracted in its place.  With DG_EXP2_INST exp2 is the part's
+ * v_exp_f32, mn = max(m, RN32(max_t score_t * qk_scale)) and p_t =
+ * exp2(fma(score_t, qk_scale, -mn)), and qk_scale has to be above 0.  So the
+ * bits of a row depend on its query, the keys that it sees and the
+ * descriptor, not on the batch, the chunk that it came in, the pages or the
+ * launch, and with split_keys 0 and DG_EXP2_LIB are dg_attention's.
+ *   Q: device, rows x q_heads x dim of q_dtype, strides in elements of whole
+ *   16-byte pieces;  O: the same rows of the descriptor's out_dtype (written,
+ *   never read; may not overlap the inputs, nor its rows each other).
+ *   cu_q (batch + 1), kv_len (batch), page_table (batch rows of table_stride,
+ *   table_width used): device int32.  max_q and max_kv: at least the most new
+ *   tokens and keys of any sequence (they size the launch: what a sequence has
+ *   beyond them is left out).
+ *   A row that sees no key is +0.  Rows before cu_q[0] or from cu_q[batch] on
+ *   are left as they are.  A page number outside the cache makes the rows that
+ *   see its keys NaN; lengths beyond the table or the batch are cut.
+ *   workspace: device, at least dg_attention_paged_bytes, 16-byte aligned, not
+ *   in use by another call or graph at the same time; or NULL: a library-owned
+ *   workspace of the (device, stream), and under capture or without memory for
+ *   it none, with one workgroup for all the spans of a row (the same bits).
+ * rows, batch or q_heads of 0 is a no-op.  One launch, two for a batch of one
+ * token and longer sequences, and one more to join spans.
+ * DG_ERR_UNSUPPORTED unless key_block is 64, block_sum DG_TREE, pv_fma 1,
+ * q_block (causal) a multiple of 64, dim 64 or 128, (q_dtype, cache, p_dtype)
+ * are (bf16, bf16, bf16), (f16, f16, f16) or (bf16, e4m3, bf16);  DG_ERR_SHAPE
+ * for sizes out of range (rows * q_heads, max_kv and table_width * page below
+ * 2^31 - 1024, batch at most 65535, q_heads a multiple of the cache's heads),
+ * DG_ERR_ALIGN, DG_ERR_INVALID as elsewhere;  DG_ERR_SCRATCH for a
+ * workspace that is too small. */
+dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void* Q, int64_t q_token, int64_t q_head,
+                             const dg_kv_cache* c, const int32_t* cu_q, const int32_t* kv_len,
+                             const int32_t* page_table, int64_t table_width, int64_t table_stride, void* O,
+                             int64_t o_token, int64_t o_head, int64_t rows, int64_t q_heads, int64_t batch,
+                             int64_t max_q, int64_t max_kv, float qk_scale, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that such a call takes (0: none; also for a call that is refused). */
+size_t dg_attention_paged_bytes(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, int64_t q_heads,
+                                int64_t batch, int64_t max_q, int64_t max_kv);
+
 /* Static text for a status code (never NULL; unknown codes give
  * "unknown status"). */
 const char* dg_strerror(dg_status s);
@@ -552,7 +695,9 @@ const char* dg_strerror(dg_status s);
  * (DG_IN_BF16_E4M3, dg_packed_b8_bytes, dg_pack_b8).  0.5.1 (501) added knob
  * kernel 12 (tile chain and tree, fma = 0, on a tiled kernel).  0.6.0 (600)
  * added e4m3 x e4m3 (DG_IN_E4M3, the DG_MMA_*_FP8 and _F8F6F4
- * instructions) and knob kernel 13. */
+ * instructions) and knob kernel 13.  The rotation, cache and paged attention
+ * entry points, and dg_attn_params.split_keys and exp2, are additions to it: a
+ * caller built against an earlier header of this version stays as it was. */
 int32_t dg_version(void);
 
 #ifdef __cplusplus

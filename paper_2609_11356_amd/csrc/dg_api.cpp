@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
+#include <cstddef>
 #include <cstdio>
 #include <cstring>
 #include <map>
@@ -1198,19 +1200,28 @@ dg_status dg_rmsnorm(const dg_desc* d, const float* X, const void* w, float eps,
   return DG_OK;
 }
 
-dg_status dg_attn_desc_create(const dg_attn_params* p, dg_attn_desc** out) {
-  if (!p || !out) return DG_ERR_INVALID;
+dg_status dg_attn_desc_create(const dg_attn_params* in_p, dg_attn_desc** out) {
+  if (!in_p || !out) return DG_ERR_INVALID;
   *out = nullptr;
-  if (p->struct_size < sizeof(dg_attn_params)) return DG_ERR_INVALID;
+  // a caller of the struct without the paged fields
+  dg_attn_params q;
+  std::memset(&q, 0, sizeof q);
+  constexpr uint32_t first_size = offsetof(dg_attn_params, split_keys);
+  if (in_p->struct_size == first_size) std::memcpy(&q, in_p, first_size);
+  else if (in_p->struct_size >= sizeof(dg_attn_params)) q = *in_p;
+  else return DG_ERR_INVALID;
+  const dg_attn_params* p = &q;
   if (p->key_block < 1 || !in(p->causal, 0, 1) || (p->causal && p->q_block < 1)) return DG_ERR_INVALID;
   if (p->block_sum != DG_SEQ && p->block_sum != DG_TREE) return DG_ERR_INVALID;
-  if (!in(p->p_dtype, DG_F32, DG_BF16) || !in(p->pv_fma, 0, 1) || !in(p->l_fma, 0, 1)) return DG_ERR_INVALID;
-  if (!in(p->final_div, DG_ATTN_DIV, DG_ATTN_RECIP) || !in(p->out_dtype, DG_F32, DG_BF16)) return DG_ERR_INVALID;
-  // the bf16 instruction takes the probabilities at bf16; the kernel's blocks
+  if (!in(p->p_dtype, DG_F32, DG_F16) || !in(p->pv_fma, 0, 1) || !in(p->l_fma, 0, 1)) return DG_ERR_INVALID;
+  if (!in(p->final_div, DG_ATTN_DIV, DG_ATTN_RECIP) || !in(p->out_dtype, DG_F32, DG_F16)) return DG_ERR_INVALID;
+  if (p->split_keys < 0 || !in(p->exp2, DG_EXP2_LIB, DG_EXP2_INST)) return DG_ERR_INVALID;
+  // the matrix instructions take the probabilities at 16 bits; the kernel's blocks
   // are whole 32-key instruction steps; a workgroup's 16-row waves share one split
-  if (p->p_dtype != DG_BF16) return DG_ERR_UNSUPPORTED;
+  if (p->p_dtype == DG_F32) return DG_ERR_UNSUPPORTED;
   if (p->key_block != 32 && p->key_block != 64 && p->key_block != 128) return DG_ERR_UNSUPPORTED;
   if (p->causal && p->q_block % 16 != 0) return DG_ERR_UNSUPPORTED;
+  if (p->split_keys % p->key_block != 0) return DG_ERR_UNSUPPORTED;
   dg_attn_desc* d = new (std::nothrow) dg_attn_desc;
   if (!d) return DG_ERR_NOMEM;
   d->p = *p;
@@ -1227,6 +1238,9 @@ dg_status dg_attention(const dg_attn_desc* d, const void* Q, const void* K, cons
   if (!d) return DG_ERR_INVALID;
   if (H < 0 || Lq < 0 || Lk < 0 || dim < 0) return DG_ERR_SHAPE;
   if (!dg::attn_supported(dim, d->p.key_block)) return DG_ERR_UNSUPPORTED;
+  // the orders that only the paged form has
+  if (d->p.p_dtype == DG_F16 || d->p.out_dtype == DG_F16 || d->p.split_keys || d->p.exp2 != DG_EXP2_LIB)
+    return DG_ERR_UNSUPPORTED;
   if (H == 0 || Lq == 0) return DG_OK;
   if (Lk < 1 || H > 65535 || (d->p.causal && Lq != Lk)) return DG_ERR_SHAPE;
   if ((Lq + 15) / 16 > 65535) return DG_ERR_SHAPE;
@@ -1260,6 +1274,346 @@ dg_status dg_attention(const dg_attn_desc* d, const void* Q, const void* K, cons
     }
   }
   if (dg::launch_attention(a, dim, d->p.key_block, st) != hipSuccess) return DG_ERR_HIP;
+  return DG_OK;
+}
+
+// --------------------------------------- positions, the paged cache
+
+dg_status dg_rope_desc_create(const dg_rope_params* p, dg_rope_desc** out) {
+  if (!p || !out) return DG_ERR_INVALID;
+  *out = nullptr;
+  if (p->struct_size < sizeof(dg_rope_params)) return DG_ERR_INVALID;
+  if (!in(p->dim, 2, DG_ROPE_MAX_DIM) || p->dim % 2 || !in(p->rotary, 2, p->dim) || p->rotary % 2) return DG_ERR_INVALID;
+  if (!in(p->pairing, DG_ROPE_HALF, DG_ROPE_ADJACENT) || !in(p->n_axes, 1, DG_ROPE_MAX_AXES)) return DG_ERR_INVALID;
+  if (!p->pair_axis && p->n_axes != 1) return DG_ERR_INVALID;
+  dg_rope_desc d;
+  std::memset(&d, 0, sizeof d);
+  d.p = *p;
+  d.p.struct_size = sizeof(dg_rope_params);
+  d.p.pair_axis = nullptr;
+  for (int i = 0; p->pair_axis && i < p->rotary / 2; ++i) {
+    if (p->pair_axis[i] >= p->n_axes) return DG_ERR_INVALID;
+    d.axis[i >> 4] |= (uint32_t)p->pair_axis[i] << (2 * (i & 15));
+  }
+  dg_rope_desc* made = new (std::nothrow) dg_rope_desc(d);
+  if (!made) return DG_ERR_NOMEM;
+  *out = made;
+  return DG_OK;
+}
+
+void dg_rope_desc_destroy(dg_rope_desc* d) { delete d; }
+
+namespace {
+
+// Rows of T tokens x H heads x dim elements at these strides.
+struct Rows {
+  const void* p;
+  int64_t token, head, T, H, dim, size;   // size: bytes per element
+  int64_t extent() const { return ((T - 1) * token + (H - 1) * head + dim) * size; }
+  bool apart() const {                    // no two rows share an element
+    const int64_t t = T > 1 ? token : INT64_MAX, h = H > 1 ? head : INT64_MAX;
+    if (t < dim || h < dim) return false;
+    if (T <= 1 || H <= 1) return true;
+    return t >= (H - 1) * h + dim || h >= (T - 1) * t + dim;
+  }
+  bool pieces() const {                   // every row starts at a 16-byte piece
+    return aligned(p, 16) && token * size % 16 == 0 && head * size % 16 == 0;
+  }
+};
+
+// Strides small enough that no offset overflows.
+bool stride_ok(int64_t s) { return s >= 0 && s < ((int64_t)1 << 40); }
+
+// Whether Y may be written while X is read: the very same rows, or none of them.
+bool in_place_or_apart(const Rows& X, const Rows& Y) {
+  if (X.p == Y.p) return (X.T <= 1 || X.token == Y.token) && (X.H <= 1 || X.head == Y.head);
+  const char *x = (const char*)X.p, *y = (const char*)Y.p;
+  return x + X.extent() <= y || y + Y.extent() <= x;
+}
+
+dg_status check_turned(const Rows& X, const Rows& Y) {
+  if (!stride_ok(X.token) || !stride_ok(X.head) || !stride_ok(Y.token) || !stride_ok(Y.head)) return DG_ERR_SHAPE;
+  if (!X.p || !Y.p) return DG_ERR_INVALID;
+  if (!aligned(X.p, X.size) || !aligned(Y.p, Y.size)) return DG_ERR_ALIGN;
+  if (!Y.apart() || !in_place_or_apart(X, Y)) return DG_ERR_INVALID;
+  return DG_OK;
+}
+
+dg_status check_tables(const int32_t* pos, const float* cos_t, const float* sin_t, int64_t table_rows) {
+  if (table_rows < 0 || table_rows > INT32_MAX) return DG_ERR_SHAPE;
+  if (!pos || !cos_t || !sin_t) return DG_ERR_INVALID;
+  return aligned(pos, 4) && aligned(cos_t, 4) && aligned(sin_t, 4) ? DG_OK : DG_ERR_ALIGN;
+}
+
+void rotation_args(const dg_rope_desc* d, const int32_t* pos, const float* cos_t, const float* sin_t,
+                   int64_t table_rows, dg::RopeArgs* a) {
+  a->pos = pos;
+  a->cos_t = cos_t;
+  a->sin_t = sin_t;
+  a->table_rows = table_rows;
+  a->dim = d->p.dim;
+  a->half = d->p.rotary / 2;
+  a->adjacent = d->p.pairing == DG_ROPE_ADJACENT;
+  a->n_axes = d->p.n_axes;
+  std::memcpy(a->axis, d->axis, sizeof a->axis);
+}
+
+// Whether the units of 16-byte pieces fit the rotation (pv pairs per unit).
+bool wide_rotation(const dg::RopeArgs& a, int pv) {
+  return a.half % pv == 0 && (a.dim - 2 * a.half) % pv == 0 && (!a.half || (aligned(a.cos_t, 16) && aligned(a.sin_t, 16)));
+}
+
+dg_status check_cache(const dg_kv_cache* c) {
+  if (!c || c->struct_size < sizeof(dg_kv_cache)) return DG_ERR_INVALID;
+  if (c->dtype != DG_BF16 && c->dtype != DG_F16 && c->dtype != DG_E4M3) return DG_ERR_INVALID;
+  if (c->pages < 1 || c->page < 1 || c->heads < 1 || c->dim < 1 || c->pages > INT32_MAX || c->page > INT32_MAX ||
+      c->heads > 65535 || c->dim > DG_ROPE_MAX_DIM)
+    return DG_ERR_SHAPE;
+  if (!stride_ok(c->page_stride) || !stride_ok(c->token_stride) || !stride_ok(c->head_stride)) return DG_ERR_SHAPE;
+  if (!c->K || !c->V) return DG_ERR_INVALID;
+  const int64_t size = c->dtype == DG_E4M3 ? 1 : 2;
+  if (!aligned(c->K, 16) || !aligned(c->V, 16) || c->page_stride * size % 16 || c->token_stride * size % 16 ||
+      c->head_stride * size % 16)
+    return DG_ERR_ALIGN;
+  if (!(c->k_scale > 0.f) || !(c->v_scale > 0.f) || std::isinf(c->k_scale) || std::isinf(c->v_scale)) return DG_ERR_INVALID;
+  if (c->dtype != DG_E4M3 && (c->k_scale != 1.f || c->v_scale != 1.f)) return DG_ERR_INVALID;
+  return DG_OK;
+}
+
+}  // namespace
+
+dg_status dg_rope(const dg_rope_desc* d, int32_t dtype, const void* X, int64_t x_token, int64_t x_head, void* Y,
+                  int64_t y_token, int64_t y_head, const int32_t* pos, const float* cos_t, const float* sin_t,
+                  int64_t table_rows, int64_t T, int64_t H, int32_t inverse, void* stream) {
+  if (!d || !in(dtype, DG_F32, DG_F16) || !in(inverse, 0, 1)) return DG_ERR_INVALID;
+  if (T < 0 || H < 0 || T > INT32_MAX || H > 65535) return DG_ERR_SHAPE;
+  if (T == 0 || H == 0) return DG_OK;
+  const int64_t size = dtype == DG_F32 ? 4 : 2;
+  const Rows x{X, x_token, x_head, T, H, d->p.dim, size}, y{Y, y_token, y_head, T, H, d->p.dim, size};
+  dg_status s = check_turned(x, y);
+  if (s == DG_OK) s = check_tables(pos, cos_t, sin_t, table_rows);
+  if (s != DG_OK) return s;
+  dg::RopeArgs a;
+  std::memset(&a, 0, sizeof a);
+  rotation_args(d, pos, cos_t, sin_t, table_rows, &a);
+  a.q = dg::RopeHeads{X, Y, x_token, x_head, y_token, y_head, (int32_t)H};
+  a.T = T;
+  a.inverse = inverse;
+  a.in_dtype = dtype;
+  const bool wide = x.pieces() && y.pieces() && wide_rotation(a, dtype == DG_F32 ? 4 : 8);
+  return dg::launch_rope(a, wide, (hipStream_t)stream) == hipSuccess ? DG_OK : DG_ERR_HIP;
+}
+
+dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_dtype, const void* Q, int64_t q_token,
+                       int64_t q_head, void* Qout, int64_t qo_token, int64_t qo_head, int64_t q_heads, const void* K,
+                       int64_t k_token, int64_t k_head, const void* V, int64_t v_token, int64_t v_head,
+                       const int32_t* pos, const float* cos_t, const float* sin_t, int64_t table_rows,
+                       const int64_t* slots, int64_t T, void* stream) {
+  dg_status s = check_cache(c);
+  if (s != DG_OK) return s;
+  if (in_dtype != DG_BF16 && in_dtype != DG_F16) return DG_ERR_INVALID;
+  if (in_dtype != c->dtype && !(in_dtype == DG_BF16 && c->dtype == DG_E4M3)) return DG_ERR_UNSUPPORTED;
+  if (!Q != !Qout || (Q && !r) || c->K == c->V) return DG_ERR_INVALID;
+  if (T < 0 || T > INT32_MAX || q_heads < 0 || q_heads > 65535 || (r && r->p.dim != c->dim) || c->dim % 2) return DG_ERR_SHAPE;
+  if (T == 0) return DG_OK;
+  if (!Q) q_heads = 0;
+  const Rows q{Q, q_token, q_head, T, q_heads, c->dim, 2}, qo{Qout, qo_token, qo_head, T, q_heads, c->dim, 2};
+  const Rows k{K, k_token, k_head, T, c->heads, c->dim, 2}, v{V, v_token, v_head, T, c->heads, c->dim, 2};
+  if (q_heads && (s = check_turned(q, qo)) != DG_OK) return s;
+  if (r && (s = check_tables(pos, cos_t, sin_t, table_rows)) != DG_OK) return s;
+  if (!stride_ok(k_token) || !stride_ok(k_head) || !stride_ok(v_token) || !stride_ok(v_head)) return DG_ERR_SHAPE;
+  if (!K || !V || !slots) return DG_ERR_INVALID;
+  if (!aligned(K, 2) || !aligned(V, 2) || !aligned(slots, 8)) return DG_ERR_ALIGN;
+  dg::RopeArgs a;
+  std::memset(&a, 0, sizeof a);
+  if (r) rotation_args(r, pos, cos_t, sin_t, table_rows, &a);
+  a.dim = (int32_t)c->dim;
+  a.q = dg::RopeHeads{Q, Qout, q_token, q_head, qo_token, qo_head, (int32_t)q_heads};
+  a.k = dg::RopeHeads{K, c->K, k_token, k_head, 0, 0, (int32_t)c->heads};
+  a.v = dg::RopeHeads{V, c->V, v_token, v_head, 0, 0, (int32_t)c->heads};
+  a.slots = slots;
+  a.T = T;
+  a.in_dtype = in_dtype;
+  a.kv_dtype = c->dtype;
+  a.page_stride = c->page_stride;
+  a.token_stride = c->token_stride;
+  a.head_stride = c->head_stride;
+  a.n_slots = c->pages * c->page;
+  a.page_size = (int32_t)c->page;
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
+  // the cache's rows are whole pieces already (check_cache)
+  const bool wide = (!q_heads || (q.pieces() && qo.pieces())) && k.pieces() && v.pieces() && wide_rotation(a, 8);
+  return dg::launch_rope(a, wide, (hipStream_t)stream) == hipSuccess ? DG_OK : DG_ERR_HIP;
+}
+
+namespace {
+
+constexpr int64_t PAGED_SIZES = INT32_MAX - 1024;         // rows * heads and keys: 31-bit counts with room
+constexpr size_t PAGED_WORKSPACE = (size_t)1 << 30;       // more records than this: one walk per row
+
+// How a paged call is run (speed only): up to two launches, for sequences of
+// few rows and for the others, each with its spans apart (records) or walked
+// by one workgroup.
+struct PagedLaunch {
+  int nw, rw;
+  int32_t row_lo, row_hi, rec_rows;
+  bool split;
+  size_t records;            // rows that have records
+};
+struct PagedPlan {
+  PagedLaunch l[2];
+  int n;
+  int32_t nspan;
+  size_t bytes;
+};
+
+PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, int64_t q_heads, int64_t batch,
+                     int64_t max_q, int64_t max_kv) {
+  PagedPlan p;
+  std::memset(&p, 0, sizeof p);
+  const int64_t g = q_heads / c->heads, most = max_q * g, split = d->p.split_keys;
+  p.nspan = split ? (int32_t)((max_kv + split - 1) / split) : 1;
+  const bool spans = p.nspan > 1 && p.nspan <= 65535;
+  if (most <= 16 || batch > 1) {
+    PagedLaunch& l = p.l[p.n++];
+    l = PagedLaunch{1, 16, 0, 16, (int32_t)std::min<int64_t>(most, 16), spans, 0};
+    l.records = (size_t)batch * c->heads * l.rec_rows;
+  }
+  if (most > 16) {
+    PagedLaunch& l = p.l[p.n++];
+    l = PagedLaunch{4, 16, p.n > 1 ? 16 : 0, INT32_MAX, 0, false, 0};
+    // workgroups of 64 rows fill the chip's 512 places, or their spans do
+    const int64_t tiles = std::min((rows * g + 63) / 64 + batch, (most + 63) / 64 * batch);
+    l.split = spans && tiles * c->heads < 512;
+    l.records = (size_t)rows * q_heads;
+  }
+  for (int i = 0; i < p.n; ++i) {
+    const size_t bytes = p.l[i].records * p.nspan * (c->dim + 2) * sizeof(float);
+    if (p.l[i].split && p.bytes + bytes > PAGED_WORKSPACE) p.l[i].split = false;
+    if (p.l[i].split) p.bytes += (bytes + 255) / 256 * 256;
+  }
+  return p;
+}
+
+dg_status check_paged(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, int64_t q_heads, int64_t batch,
+                      int64_t max_q, int64_t max_kv) {
+  if (!d) return DG_ERR_INVALID;
+  dg_status s = check_cache(c);
+  if (s != DG_OK) return s;
+  if (rows < 0 || q_heads < 0 || batch < 0 || max_q < 0 || max_kv < 0) return DG_ERR_SHAPE;
+  const dg_attn_params& p = d->p;
+  if (p.key_block != 64 || p.block_sum != DG_TREE || !p.pv_fma || (p.causal && p.q_block % 64)) return DG_ERR_UNSUPPORTED;
+  if (c->dim != 64 && c->dim != 128) return DG_ERR_UNSUPPORTED;
+  if (p.p_dtype != (c->dtype == DG_F16 ? DG_F16 : DG_BF16)) return DG_ERR_UNSUPPORTED;
+  if (rows > PAGED_SIZES || q_heads > 65535 || rows * q_heads > PAGED_SIZES || batch > 65535 || max_kv > PAGED_SIZES ||
+      q_heads % c->heads)
+    return DG_ERR_SHAPE;
+  return DG_OK;
+}
+
+}  // namespace
+
+size_t dg_attention_paged_bytes(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, int64_t q_heads,
+                                int64_t batch, int64_t max_q, int64_t max_kv) {
+  if (check_paged(d, c, rows, q_heads, batch, max_q, max_kv) != DG_OK || rows == 0 || q_heads == 0 || batch == 0) return 0;
+  return paged_plan(d, c, rows, q_heads, batch, std::min(max_q, rows), max_kv).bytes;
+}
+
+dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void* Q, int64_t q_token, int64_t q_head,
+                             const dg_kv_cache* c, const int32_t* cu_q, const int32_t* kv_len,
+                             const int32_t* page_table, int64_t table_width, int64_t table_stride, void* O,
+                             int64_t o_token, int64_t o_head, int64_t rows, int64_t q_heads, int64_t batch,
+                             int64_t max_q, int64_t max_kv, float qk_scale, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  dg_status s = check_paged(d, c, rows, q_heads, batch, max_q, max_kv);
+  if (s != DG_OK) return s;
+  if (q_dtype != (c->dtype == DG_F16 ? DG_F16 : DG_BF16)) return DG_ERR_UNSUPPORTED;
+  if (table_width < 0 || !stride_ok(table_stride) || (batch > 1 && table_stride < table_width)) return DG_ERR_SHAPE;
+  if (table_width > PAGED_SIZES / c->page) return DG_ERR_SHAPE;
+  if (!stride_ok(q_token) || !stride_ok(q_head) || !stride_ok(o_token) || !stride_ok(o_head)) return DG_ERR_SHAPE;
+  // the instruction's form takes the largest score times the scale as the largest product
+  if (d->p.exp2 == DG_EXP2_INST && !(qk_scale > 0.f)) return DG_ERR_INVALID;
+  if (rows == 0 || q_heads == 0 || batch == 0) return DG_OK;
+  if (!Q || !O || !cu_q || !kv_len || (!page_table && table_width > 0)) return DG_ERR_INVALID;
+  const Rows q{Q, q_token, q_head, rows, q_heads, c->dim, 2};
+  const Rows o{O, o_token, o_head, rows, q_heads, c->dim, d->p.out_dtype == DG_F32 ? 4 : 2};
+  if (!q.pieces() || !o.pieces() || !aligned(cu_q, 4) || !aligned(kv_len, 4) || !aligned(page_table, 4)) return DG_ERR_ALIGN;
+  if (!o.apart() || (const char*)Q == (const char*)O) return DG_ERR_INVALID;
+  max_q = std::min(max_q, rows);
+  if (max_q == 0) return DG_OK;
+  dg::PagedArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.Q = (const uint16_t*)Q;
+  a.O = O;
+  a.K = c->K;
+  a.V = c->V;
+  a.cu_q = cu_q;
+  a.kv_len = kv_len;
+  a.page_table = page_table;
+  a.q_token = q_token;
+  a.q_head = q_head;
+  a.o_token = o_token;
+  a.o_head = o_head;
+  const int64_t size = c->dtype == DG_E4M3 ? 1 : 2;
+  a.page_stride = c->page_stride * size;
+  a.token_stride = c->token_stride * size;
+  a.head_stride = c->head_stride * size;
+  a.table_stride = table_stride;
+  a.dim = (int32_t)c->dim;
+  a.rows = (int32_t)rows;
+  a.B = (int32_t)batch;
+  a.Hkv = (int32_t)c->heads;
+  a.g = (int32_t)(q_heads / c->heads);
+  a.pages = (int32_t)c->pages;
+  a.page_size = (int32_t)c->page;
+  a.kv_cap = (int32_t)std::min(max_kv, table_width * c->page);
+  // key / page for key < 2^31: with 2^(s - 1) < page <= 2^s and mul = floor(2^(31 + s)
+  // / page) + 1 the product is off by less than 2^(31 + s) / page, as mul * page
+  // exceeds 2^(31 + s) by at most page <= 2^s
+  while (((int64_t)1 << a.page_shift) < c->page) ++a.page_shift;
+  a.page_shift += 31;
+  a.page_mul = (uint32_t)((((uint64_t)1 << a.page_shift) / (uint64_t)c->page) + 1);
+  a.max_q = (int32_t)max_q;
+  a.span_blocks = d->p.split_keys / 64;
+  a.causal = d->p.causal;
+  a.l_fma = d->p.l_fma;
+  a.final_recip = d->p.final_div == DG_ATTN_RECIP;
+  a.out_dtype = d->p.out_dtype;
+  a.kv_dtype = c->dtype;
+  a.inst = d->p.exp2 == DG_EXP2_INST;
+  a.qk_scale = qk_scale * c->k_scale;
+  a.v_scale = c->v_scale;
+  hipStream_t st = (hipStream_t)stream;
+  PagedPlan plan = paged_plan(d, c, rows, q_heads, batch, max_q, max_kv);
+  a.nspan = plan.nspan;
+  void* ws = nullptr;
+  Lease lease;
+  if (plan.bytes && workspace) {
+    if (workspace_bytes < plan.bytes) return DG_ERR_SCRATCH;
+    if (!aligned(workspace, 16)) return DG_ERR_ALIGN;
+    ws = workspace;
+  } else if (plan.bytes && (capturing(st) || get_workspace(st, plan.bytes, &ws, &lease, WS_ATTENTION) != DG_OK)) {
+    ws = nullptr;   // one workgroup per row tile walks all the spans
+  }
+  char* at = (char*)ws;
+  dg::PagedArgs part[2];
+  for (int i = 0; i < plan.n; ++i) {
+    const PagedLaunch& l = plan.l[i];
+    dg::PagedArgs& b = part[i] = a;
+    b.row_lo = l.row_lo;
+    b.row_hi = l.row_hi;
+    if (l.split && ws) {
+      const size_t n = l.records * plan.nspan;
+      b.rec_rows = l.rec_rows;
+      b.rec = (float*)at;
+      b.rec_ml = (float2*)(at + n * c->dim * sizeof(float));
+      at += (n * (c->dim + 2) * sizeof(float) + 255) / 256 * 256;
+    }
+    if (dg::launch_attention_paged(b, l.nw, l.rw, st) != hipSuccess) return DG_ERR_HIP;
+  }
+  for (int i = 0; i < plan.n; ++i)
+    if (part[i].rec && dg::launch_attention_paged_join(part[i], st) != hipSuccess) return DG_ERR_HIP;
   return DG_OK;
 }
 

@@ -34,6 +34,18 @@ __device__ __forceinline__ uint32_t f32x2_bf16x2(float lo, float hi) {
 
 __device__ __forceinline__ float round_bf16(float x) { return bf16_f32(f32_bf16(x)); }
 
+// OCP e4m3 byte(s) widened to bf16 by the part's own conversion (exact:
+// every e4m3 value, subnormals and signed zeros included, is a bf16 value;
+// NaN stays NaN), the pair in bytes 2h and 2h + 1 of x.
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t x) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.0f, HI));
+}
+__device__ __forceinline__ uint16_t e4m3_bf16(uint8_t b) {
+  return (uint16_t)(e4m3x2_bf16x2<false>(b) & 0xffffu);
+}
+
 // exp(x) in binary32 by a fixed sequence of steps (Cody & Waite reduction,
 // Taylor polynomial, exact power-of-two scaling):
 //   n  = rint(x * log2 e)

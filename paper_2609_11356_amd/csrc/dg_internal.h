@@ -17,6 +17,11 @@ struct dg_attn_desc {
   dg_attn_params p;            // validated copy
 };
 
+struct dg_rope_desc {
+  dg_rope_params p;            // validated copy; pair_axis is not kept
+  uint32_t axis[16];           // the axis of each pair, two bits
+};
+
 namespace dg {
 
 // Everything a GEMM launch needs, passed by value as the kernel argument.
@@ -90,6 +95,56 @@ struct AttnArgs {
   int32_t causal, q_block;
   int32_t block_tree, pv_fma, l_fma, final_recip, out_bf16;
 };
+
+// Attention over a paged cache (dg_attn_paged.hip), by value to its kernels.
+struct PagedArgs {
+  const uint16_t* Q;             // rows x heads x d, bf16 or binary16, strides in elements
+  void* O;                       // the same rows of out_dtype
+  const void* K;                 // the cache: strides in bytes
+  const void* V;
+  const int32_t* cu_q;           // B + 1
+  const int32_t* kv_len;         // B
+  const int32_t* page_table;     // B rows of table_stride
+  int64_t q_token, q_head, o_token, o_head;
+  int64_t page_stride, token_stride, head_stride, table_stride;
+  float* rec;                    // the spans' O records ([row][nspan][d]), or null: one walk over all
+  float2* rec_ml;                // and their (m, l)
+  int32_t dim, rows, B, Hkv, g;
+  int32_t pages, page_size, kv_cap;   // kv_cap: keys that the batch's lengths are cut to
+  uint32_t page_mul, page_shift;      // key / page_size = key * page_mul >> page_shift (key < 2^31)
+  int32_t max_q, span_blocks, nspan;  // blocks of 64 keys per span; spans of max_kv keys
+  int32_t row_lo, row_hi;        // sequences with row_lo < new tokens * g <= row_hi are taken
+  int32_t rec_rows;              // records of row r of (sequence, key head): rows reserved for each; 0: by token and head
+  int32_t causal, l_fma, final_recip, out_dtype, kv_dtype, inst;
+  float qk_scale, v_scale;
+};
+
+// nw waves of rw rows per workgroup: (1, 16), (4, 16) or (4, 32)
+hipError_t launch_attention_paged(const PagedArgs& a, int nw, int rw, hipStream_t s);
+hipError_t launch_attention_paged_join(const PagedArgs& a, hipStream_t s);
+
+// Rotary positions and the cache append (dg_rope.hip).
+struct RopeHeads {               // T tokens x heads x dim, strides in elements
+  const void* X;
+  void* Y;
+  int64_t x_token, x_head, y_token, y_head;
+  int32_t heads;
+};
+struct RopeArgs {
+  RopeHeads q, k, v;             // rotated to Y; rotated into the cache; copied into the cache
+  const int32_t* pos;            // n_axes x T
+  const float* cos_t;            // table_rows x half
+  const float* sin_t;
+  const int64_t* slots;          // T (append)
+  int64_t T, table_rows;
+  int32_t dim, half, adjacent, n_axes, inverse;
+  int32_t in_dtype, kv_dtype, append;
+  int64_t page_stride, token_stride, head_stride, n_slots;   // the cache, in elements
+  int32_t page_size;
+  float k_scale, v_scale;
+  uint32_t axis[16];             // two bits per pair
+};
+hipError_t launch_rope(const RopeArgs& a, bool wide, hipStream_t s);
 
 bool attn_supported(int64_t d, int key_block);
 hipError_t launch_attention(const AttnArgs& a, int64_t d, int key_block, hipStream_t s);

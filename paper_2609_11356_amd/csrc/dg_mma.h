@@ -65,18 +65,6 @@ __device__ __forceinline__ void finish(const GemmArgs& a, int s, int64_t i, int6
   else ((float*)a.C)[i * a.N + j] = z;
 }
 
-// OCP e4m3 byte(s) widened to bf16 by the part's own conversion (exact:
-// every e4m3 value, subnormals and signed zeros included, is a bf16 value;
-// NaN stays NaN), the pair in bytes 2h and 2h + 1 of x.
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-template <bool HI>
-__device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t x) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, 1.0f, HI));
-}
-__device__ __forceinline__ uint16_t e4m3_bf16(uint8_t b) {
-  return (uint16_t)(e4m3x2_bf16x2<false>(b) & 0xffffu);
-}
-
 // s_waitcnt immediate waiting for at most n outstanding vector-memory
 // operations (gfx9 encoding: vmcnt[3:0] in bits 3:0, vmcnt[5:4] in bits
 // 15:14; expcnt 7 and lgkmcnt 15 mean no wait on those counters).

@@ -1,0 +1,210 @@
+// dg_rope.hip -- rotary positions, and appending keys and values to a paged
+// cache with the rotation on the way.
+//
+// Pair i of a head, (x1, x2) = (x_i, x_{i + half}) or (x_2i, x_{2i + 1}), is
+// turned by the angle whose cosine and sine stand in row pos[axis_i, t] of the
+// tables:  y1 = RN(RN(x1 c) - RN(x2 s)),  y2 = RN(RN(x2 c) + RN(x1 s)), then
+// rounded once to the output's type; the inverse takes -s, which is the
+// gradient too.  A position outside the tables turns by NaN.
+//
+// Bound: HBM.  A thread takes a unit of 2 PV elements of a head, PV pairs
+// (16-byte loads and stores), for up to HPT heads, so that the cosines and
+// sines of a unit are fetched once for all of them.
+#include "dg_device.h"
+#include "dg_internal.h"
+
+namespace dg {
+namespace {
+
+template <typename T, int N>
+struct alignas(N * sizeof(T) >= 16 ? 16 : N * sizeof(T)) Pack {
+  T v[N];
+};
+
+__device__ __forceinline__ float widen(uint16_t x, int32_t dtype) {
+  return dtype == DG_BF16 ? bf16_f32(x) : (float)__builtin_bit_cast(_Float16, x);
+}
+__device__ __forceinline__ float widen(float x, int32_t) { return x; }
+
+template <int N>
+__device__ __forceinline__ void put(float* p, const float* y, int32_t) {
+  Pack<float, N> o;
+#pragma unroll
+  for (int e = 0; e < N; ++e) o.v[e] = y[e];
+  *(Pack<float, N>*)p = o;
+}
+template <int N>
+__device__ __forceinline__ void put(uint16_t* p, const float* y, int32_t dtype) {
+  Pack<uint16_t, N> o;
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    o.v[e] = dtype == DG_BF16 ? f32_bf16(y[e]) : __builtin_bit_cast(uint16_t, (_Float16)y[e]);
+  *(Pack<uint16_t, N>*)p = o;
+}
+
+// y / scale rounded once to e4m3, cut to +-448 (a NaN stays one).
+__device__ __forceinline__ uint8_t f32_e4m3(float y, float scale) {
+  float x = y / scale;
+  x = x > 448.0f ? 448.0f : x < -448.0f ? -448.0f : x;
+  return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
+}
+
+// N elements of a row of the cache at element offset `at`.
+template <int N>
+__device__ __forceinline__ void put_cache(void* base, int64_t at, const float* y, int32_t dtype, float scale) {
+  if (dtype == DG_E4M3) {
+    Pack<uint8_t, N> o;
+#pragma unroll
+    for (int e = 0; e < N; ++e) o.v[e] = f32_e4m3(y[e], scale);
+    *(Pack<uint8_t, N>*)((uint8_t*)base + at) = o;
+  } else put<N>((uint16_t*)base + at, y, dtype);
+}
+
+}  // namespace
+
+// E: the element type's storage (uint16_t, or float without a cache); PV: pairs
+// per unit; HPT: heads per thread.  A head has u_rot units that turn and u_rest
+// of 2 PV elements behind them (the last one shorter).  `heads` counts the head
+// groups of q, then k, then v.
+template <typename E, int PV, int HPT>
+__global__ __launch_bounds__(256) void rope(RopeArgs a, int tokens, int gq, int gk, int units) {
+  const int groups = gq + 2 * gk, per = groups * units;      // threads of a token
+  const int u_rot = (a.half + PV - 1) / PV;
+  for (int w = threadIdx.x; w < tokens * per; w += 256) {
+    const int64_t t = (int64_t)blockIdx.x * tokens + w / per;
+    if (t >= a.T) break;
+    const int gr = w % per / units, u = w % units;
+    const bool is_q = gr < gq, is_v = gr >= gq + gk;
+    const RopeHeads& h = is_q ? a.q : is_v ? a.v : a.k;
+    const int head0 = (is_q ? gr : is_v ? gr - gq - gk : gr - gq) * HPT;
+    int64_t at = 0;
+    if (!is_q) {
+      const int64_t slot = a.slots[t];
+      if (slot < 0 || slot >= a.n_slots) continue;
+      const int64_t page = slot / a.page_size;
+      at = page * a.page_stride + (slot - page * a.page_size) * a.token_stride;
+    }
+    const E* X = (const E*)h.X + t * h.x_token;
+    E* Y = (E*)h.Y + t * h.y_token;
+    const float scale = is_v ? a.v_scale : a.k_scale;
+    // where the unit's two runs of PV elements lie (adjacent pairs, and what is
+    // not turned: one run of 2 PV)
+    const bool turn = u < u_rot && !is_v;
+    const int e0 = u < u_rot ? (a.adjacent || is_v ? 2 * PV * u : PV * u) : 2 * a.half + 2 * PV * (u - u_rot);
+    const int e1 = u < u_rot && !a.adjacent && !is_v ? e0 + a.half : e0 + PV;
+    const bool second = e1 < a.dim;                          // a last short unit has one run only
+    float c[PV], s[PV];
+    if (turn) {
+      const int i0 = PV * u;
+      bool same = a.n_axes == 1;
+      if (!same) {
+        // all pairs of the unit on one axis: one position
+        const uint32_t x = a.axis[i0 >> 4] >> (2 * (i0 & 15));
+        same = true;
+#pragma unroll
+        for (int e = 1; e < PV; ++e) same = same && ((x >> (2 * e)) & 3) == (x & 3);
+      }
+      if (same) {
+        const int64_t p = a.pos[(a.n_axes == 1 ? 0 : (int64_t)((a.axis[i0 >> 4] >> (2 * (i0 & 15))) & 3) * a.T) + t];
+        const bool in = p >= 0 && p < a.table_rows;
+        Pack<float, PV> cc, ss;
+        if (in) {
+          cc = *(const Pack<float, PV>*)&a.cos_t[p * a.half + i0];
+          ss = *(const Pack<float, PV>*)&a.sin_t[p * a.half + i0];
+        }
+#pragma unroll
+        for (int e = 0; e < PV; ++e) {
+          c[e] = in ? cc.v[e] : __builtin_nanf("");
+          s[e] = in ? ss.v[e] : __builtin_nanf("");
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < PV; ++e) {
+          const int i = i0 + e;
+          const int64_t p = a.pos[(int64_t)((a.axis[i >> 4] >> (2 * (i & 15))) & 3) * a.T + t];
+          const bool in = p >= 0 && p < a.table_rows;
+          c[e] = in ? a.cos_t[p * a.half + i] : __builtin_nanf("");
+          s[e] = in ? a.sin_t[p * a.half + i] : __builtin_nanf("");
+        }
+      }
+      if (a.inverse)
+#pragma unroll
+        for (int e = 0; e < PV; ++e) s[e] = -s[e];
+    }
+    Pack<E, PV> x0[HPT], x1[HPT];
+#pragma unroll
+    for (int n = 0; n < HPT; ++n)
+      if (head0 + n < h.heads) {
+        x0[n] = *(const Pack<E, PV>*)&X[(head0 + n) * h.x_head + e0];
+        if (second) x1[n] = *(const Pack<E, PV>*)&X[(head0 + n) * h.x_head + e1];
+      }
+#pragma unroll
+    for (int n = 0; n < HPT; ++n) {
+      if (head0 + n >= h.heads) break;
+      float y0[PV], y1[PV];
+#pragma unroll
+      for (int e = 0; e < PV; ++e) {
+        y0[e] = widen(x0[n].v[e], a.in_dtype);
+        y1[e] = second ? widen(x1[n].v[e], a.in_dtype) : 0.f;
+      }
+      if (turn && a.adjacent) {
+        float z[2 * PV];
+#pragma unroll
+        for (int e = 0; e < PV; ++e) {
+          z[e] = y0[e];
+          z[PV + e] = y1[e];
+        }
+#pragma unroll
+        for (int e = 0; e < PV; ++e) {
+          const float p = z[2 * e], q = z[2 * e + 1];
+          z[2 * e] = p * c[e] - q * s[e];
+          z[2 * e + 1] = q * c[e] + p * s[e];
+        }
+#pragma unroll
+        for (int e = 0; e < PV; ++e) {
+          y0[e] = z[e];
+          y1[e] = z[PV + e];
+        }
+      } else if (turn) {
+#pragma unroll
+        for (int e = 0; e < PV; ++e) {
+          const float p = y0[e], q = y1[e];
+          y0[e] = p * c[e] - q * s[e];
+          y1[e] = q * c[e] + p * s[e];
+        }
+      }
+      if (is_q) {
+        E* y = Y + (head0 + n) * h.y_head;
+        put<PV>(y + e0, y0, a.in_dtype);
+        if (second) put<PV>(y + e1, y1, a.in_dtype);
+      } else {
+        const int64_t row = at + (head0 + n) * a.head_stride;
+        put_cache<PV>(h.Y, row + e0, y0, a.kv_dtype, scale);
+        if (second) put_cache<PV>(h.Y, row + e1, y1, a.kv_dtype, scale);
+      }
+    }
+  }
+}
+
+namespace {
+
+template <typename E, int PV, int HPT>
+hipError_t launch_heads(const RopeArgs& a, hipStream_t st) {
+  const int gq = (a.q.heads + HPT - 1) / HPT, gk = (a.k.heads + HPT - 1) / HPT;
+  const int units = (a.half + PV - 1) / PV + (a.dim - 2 * a.half + 2 * PV - 1) / (2 * PV);
+  const int64_t per = (int64_t)(gq + 2 * gk) * units;
+  const int tokens = per >= 256 ? 1 : (int)(256 / per);
+  const int64_t blocks = (a.T + tokens - 1) / tokens;
+  hipLaunchKernelGGL((rope<E, PV, HPT>), dim3((unsigned)blocks), dim3(256), 0, st, a, tokens, gq, gk, units);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// wide: every row, run and stride a whole number of 16-byte pieces
+hipError_t launch_rope(const RopeArgs& a, bool wide, hipStream_t st) {
+  if (a.in_dtype == DG_F32) return wide ? launch_heads<float, 4, 4>(a, st) : launch_heads<float, 1, 1>(a, st);
+  return wide ? launch_heads<uint16_t, 8, 4>(a, st) : launch_heads<uint16_t, 1, 1>(a, st);
+}
+
+}  // namespace dg

@@ -26,6 +26,10 @@ REDUCE = {"sum": 0, "sumsq": 1}
 MAX_SPLIT = 64
 SIGNATURE_MAX = 2048
 NOALLOC_SCRATCH_BYTES = 16 << 20
+# the element types of the operators on positions and the paged cache
+ELEMENT = {"f32": 0, "bf16": 1, "f16": 2, "e4m3": 3}
+PAIRING = {"half": 0, "adjacent": 1}
+EXP2 = {"lib": 0, "inst": 1}
 
 
 class DgError(RuntimeError):
@@ -53,7 +57,21 @@ class dg_knobs(ctypes.Structure):
 class dg_attn_params(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32)] + [
         (n, ctypes.c_int32) for n in ("key_block", "causal", "q_block", "block_sum", "p_dtype", "pv_fma", "l_fma",
-                                      "final_div", "out_dtype")]
+                                      "final_div", "out_dtype", "split_keys", "exp2")]
+
+
+class dg_rope_params(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (n, ctypes.c_int32) for n in ("dim", "rotary", "pairing", "n_axes")] + [
+        ("pair_axis", ctypes.POINTER(ctypes.c_uint8))]
+
+
+class dg_kv_cache(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("K", ctypes.c_void_p),
+                ("V", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("pages", "page", "heads", "dim", "page_stride", "token_stride",
+                                      "head_stride")] + [
+        ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
 
 
 _lib = None
@@ -98,6 +116,21 @@ def lib():
         L.dg_attn_desc_destroy.restype = None
         L.dg_attention.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, ctypes.c_float, vp]
         L.dg_attention.restype = ctypes.c_int
+        i32, f32 = ctypes.c_int32, ctypes.c_float
+        L.dg_rope_desc_create.argtypes = [ctypes.POINTER(dg_rope_params), ctypes.POINTER(vp)]
+        L.dg_rope_desc_create.restype = ctypes.c_int
+        L.dg_rope_desc_destroy.argtypes = [vp]
+        L.dg_rope_desc_destroy.restype = None
+        L.dg_rope.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, i64, i64, i64, i32, vp]
+        L.dg_rope.restype = ctypes.c_int
+        L.dg_kv_append.argtypes = [vp, vp, i32, vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, vp, i64, i64,
+                                   vp, vp, vp, i64, vp, i64, vp]
+        L.dg_kv_append.restype = ctypes.c_int
+        L.dg_attention_paged.argtypes = [vp, i32, vp, i64, i64, vp, vp, vp, vp, i64, i64, vp, i64, i64, i64, i64,
+                                         i64, i64, i64, f32, vp, ctypes.c_size_t, vp]
+        L.dg_attention_paged.restype = ctypes.c_int
+        L.dg_attention_paged_bytes.argtypes = [vp, vp, i64, i64, i64, i64, i64]
+        L.dg_attention_paged_bytes.restype = ctypes.c_size_t
         L.dg_strerror.argtypes = [ctypes.c_int]
         L.dg_strerror.restype = ctypes.c_char_p
         L.dg_version.restype = ctypes.c_int32
@@ -535,14 +568,20 @@ def dg_softmax(desc: Desc, X, Y, rows=None, cols=None, stream=None):
     return Y
 
 
+_ATTN_TYPE = {"f32": 0, "bf16": 1, "f16": 2}
+
+
 class AttnDesc:
     """An immutable attention descriptor (dg_attn_desc_create /
     dg_attn_desc_destroy).  Fields: key_block (BLOCK_N), causal (0/1), q_block
     (BLOCK_M, causal only), block_sum ("seq" | "tree"), p_dtype ("bf16"),
-    pv_fma (0/1), l_fma (0/1), final ("div" | "recip"), out ("f32" | "bf16")."""
+    pv_fma (0/1), l_fma (0/1), final ("div" | "recip"), out ("f32" | "bf16").
+    For dg_attention_paged also split_keys (keys per span, 0: one span), exp2
+    ("lib" | "inst": the library's exponential or the part's), and "f16" as
+    p_dtype and out."""
 
     DEFAULTS = dict(key_block=64, causal=0, q_block=64, block_sum="tree", p_dtype="bf16", pv_fma=1, l_fma=0,
-                    final="div", out="bf16")
+                    final="div", out="bf16", split_keys=0, exp2="lib")
 
     def __init__(self, **fields):
         unknown = set(fields) - set(self.DEFAULTS) - {"model"}
@@ -560,11 +599,13 @@ class AttnDesc:
         p.causal = int(f["causal"])
         p.q_block = int(f["q_block"])
         p.block_sum = COMBINE[f["block_sum"]]
-        p.p_dtype = DTYPE[f["p_dtype"]]
+        p.p_dtype = _ATTN_TYPE[f["p_dtype"]]
         p.pv_fma = int(f["pv_fma"])
         p.l_fma = int(f["l_fma"])
         p.final_div = {"div": 0, "recip": 1}[f["final"]]
-        p.out_dtype = DTYPE[f["out"]]
+        p.out_dtype = _ATTN_TYPE[f["out"]]
+        p.split_keys = int(f["split_keys"])
+        p.exp2 = EXP2[f["exp2"]]
         h = ctypes.c_void_p()
         st = lib().dg_attn_desc_create(ctypes.byref(p), ctypes.byref(h))
         if st != DG_OK:
@@ -619,10 +660,248 @@ def dg_attention(desc: AttnDesc, Q, K, V, O, qk_scale, H=None, Lq=None, Lk=None,
     return O
 
 
+class RopeDesc:
+    """An immutable rotation (dg_rope_desc_create / dg_rope_desc_destroy): dim
+    elements per head, of which the first rotary (default: all) turn in pairs
+    (pairing "half": i with i + rotary / 2, "adjacent": 2i with 2i + 1); axes,
+    for positions with several axes (time, height, width, ...), the axis of
+    each of the rotary / 2 pairs."""
+
+    def __init__(self, dim, rotary=None, pairing="half", axes=None):
+        rotary = dim if rotary is None else rotary
+        axes = None if axes is None else tuple(int(a) for a in axes)
+        _need(axes is None or (len(axes) == rotary // 2 and all(0 <= a < 256 for a in axes)),
+              "axes must name the axis of each of the %d pairs" % (rotary // 2))
+        p = dg_rope_params()
+        p.struct_size = ctypes.sizeof(dg_rope_params)
+        p.dim, p.rotary, p.pairing = int(dim), int(rotary), PAIRING[pairing]
+        p.n_axes = 1 if not axes else max(axes) + 1
+        if axes:
+            held = (ctypes.c_uint8 * len(axes))(*axes)
+            p.pair_axis = ctypes.cast(held, ctypes.POINTER(ctypes.c_uint8))
+        h = ctypes.c_void_p()
+        st = lib().dg_rope_desc_create(ctypes.byref(p), ctypes.byref(h))
+        if st != DG_OK:
+            raise DgError(st, "dg_rope_desc_create")
+        self.handle = h
+        self.dim, self.rotary, self.pairing, self.axes, self.n_axes = int(dim), int(rotary), pairing, axes, p.n_axes
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h and _lib is not None:
+            _lib.dg_rope_desc_destroy(h)
+            self.handle = None
+
+
+def _element(t):
+    """The library's number of a tensor's element type (None: it has none)."""
+    import torch
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}.get(t.dtype)
+
+
+_elements = {}     # the same by dtype, filled as types are met
+
+
+def _type_of(t):
+    n = _elements.get(t.dtype)
+    if n is None:
+        n = _element(t)
+        _need(n is not None, "%s is not an element type of this operator" % t.dtype)
+        _elements[t.dtype] = n
+    return n
+
+
+def _here(*ts):
+    """All tensors on the current device (the stream is its own)."""
+    if _tensor is None:
+        _bind_torch()
+    device = _get_device() if all(t.is_cuda for t in ts) else None
+    _need(device is not None and all(t.get_device() == device for t in ts),
+          "tensors must be on the current GPU")
+
+
+def _check_tables(desc, pos, cos, sin, T):
+    """Positions (n_axes, T) or, of one axis, (T,); returns the tables' rows."""
+    import torch
+    _need(pos.dtype is torch.int32 and pos.is_contiguous() and tuple(pos.shape) in
+          (((desc.n_axes, T),) if desc.n_axes > 1 else ((1, T), (T,))),
+          "pos must be %d x %d contiguous int32" % (desc.n_axes, T))
+    _need(cos.dtype is torch.float32 and sin.dtype is torch.float32 and cos.dim() == 2 and sin.shape == cos.shape
+          and cos.shape[1] == desc.rotary // 2 and cos.is_contiguous() and sin.is_contiguous(),
+          "cos and sin must be contiguous fp32 tables of %d columns" % (desc.rotary // 2))
+    _here(pos, cos, sin)
+    return cos.shape[0]
+
+
+def _check_heads(X, dim, name):
+    _need(X.dim() == 3 and X.shape[2] == dim and (X.stride(2) == 1 or X.numel() == 0),
+          "%s must be (tokens, heads, %d) with whole heads" % (name, dim))
+
+
+def dg_rope(desc: RopeDesc, X, pos, cos, sin, Y, inverse=False, stream=None):
+    """Y = X turned by its tokens' positions (inverse: turned back, which is the
+    gradient of X given that of Y).  X and Y (T, H, dim) bf16, float16 or
+    fp32, the heads contiguous, at any token and head strides; Y may be X.
+    pos (n_axes, T) (or (T,)) int32 rows into the fp32 tables cos and sin (rows,
+    rotary / 2)."""
+    _check_heads(X, desc.dim, "X")
+    _check_heads(Y, desc.dim, "Y")
+    _need(Y.shape == X.shape and Y.dtype is X.dtype, "Y must have X's shape and dtype")
+    T, H, _ = X.shape
+    rows = _check_tables(desc, pos, cos, sin, T)
+    _here(X, Y)
+    kind = _type_of(X)
+    _need(kind <= 2, "X must be bf16, float16 or fp32")
+    xs, ys = X.stride(), Y.stride()
+    st = lib().dg_rope(desc.handle, kind, X.data_ptr(), xs[0], xs[1], Y.data_ptr(), ys[0], ys[1], pos.data_ptr(),
+                       cos.data_ptr(), sin.data_ptr(), rows, T, H, 1 if inverse else 0, _stream(stream))
+    if st != DG_OK:
+        raise DgError(st, "dg_rope")
+    return Y
+
+
+class KvCache:
+    """A paged cache of keys and values: K and V (pages, page, heads, dim) bf16,
+    float16 or e4m3 (float8_e4m3fn or uint8), laid out alike, the heads
+    contiguous and every stride whole 16-byte pieces ((pages, heads, page, dim)
+    storage as a transposed view, too).  An e4m3 element stands for its value times
+    k_scale (v_scale).  The tensors are the caller's and are kept alive here."""
+
+    def __init__(self, K, V, k_scale=1.0, v_scale=1.0):
+        import torch
+        _need(K.dim() == 4 and V.shape == K.shape and V.stride() == K.stride() and V.dtype is K.dtype,
+              "K and V must be (pages, page, heads, dim), laid out alike")
+        _need(K.numel() > 0 and K.stride(3) == 1, "the cache must hold whole heads")
+        _here(K, V)
+        self.K, self.V = K, V
+        self.e4m3 = K.dtype in (torch.uint8, torch.float8_e4m3fn)
+        kind = 3 if self.e4m3 else _type_of(K)
+        _need(kind != 0, "the cache must be bf16, float16 or e4m3")
+        self.kind, self.device = kind, K.get_device()
+        self.pages, self.page, self.heads, self.dim = K.shape
+        c = self.struct = dg_kv_cache()
+        c.struct_size = ctypes.sizeof(dg_kv_cache)
+        c.dtype, c.K, c.V = kind, K.data_ptr(), V.data_ptr()
+        c.pages, c.page, c.heads, c.dim = K.shape
+        c.page_stride, c.token_stride, c.head_stride = K.stride()[:3]
+        c.k_scale, c.v_scale = float(k_scale), float(v_scale)
+        self.ref = ctypes.addressof(c)
+        # the type that goes in (and that attention's queries have)
+        self.in_type = torch.float16 if K.dtype is torch.float16 else torch.bfloat16
+
+
+def dg_kv_append(desc, K, V, pos, cos, sin, slots, cache: KvCache, Q=None, Qout=None, stream=None):
+    """Appends T tokens to the cache: token t's keys turned by desc (a RopeDesc, or
+    None for keys as they are; pos, cos and sin as dg_rope's) and its values to
+    slot slots[t] (int64, page * page size + place; one outside the cache is left
+    out).  K, V (T, heads, dim) of the cache's type (bf16 over e4m3); with Q (T,
+    q_heads, dim) its heads turned into Qout, which may be Q."""
+    import torch
+    _check_heads(K, cache.dim, "K")
+    _check_heads(V, cache.dim, "V")
+    T = K.shape[0]
+    kind = cache.in_type
+    _need(K.shape == V.shape and K.shape[1] == cache.heads and K.dtype is kind and V.dtype is kind,
+          "K and V must be (tokens, %d, %d) %s" % (cache.heads, cache.dim, kind))
+    _need(slots.dtype is torch.int64 and slots.is_contiguous() and tuple(slots.shape) == (T,),
+          "slots must be %d contiguous int64" % T)
+    _need((Q is None) == (Qout is None) and (Q is None or desc is not None), "Q turns into Qout by desc")
+    if _tensor is None:
+        _bind_torch()
+    _need(cache.device == _get_device(), "the cache must be on the current GPU")
+    _here(K, V, slots)
+    p = c = s = q = qo = None
+    rows = heads = 0
+    qs = qos = (0, 0)
+    if desc is not None:
+        _need(desc.dim == cache.dim, "the rotation must be of the cache's head size")
+        rows = _check_tables(desc, pos, cos, sin, T)
+        p, c, s = pos.data_ptr(), cos.data_ptr(), sin.data_ptr()
+    if Q is not None:
+        _check_heads(Q, cache.dim, "Q")
+        _check_heads(Qout, cache.dim, "Qout")
+        _need(Q.shape[0] == T and Qout.shape == Q.shape and Q.dtype is kind and Qout.dtype is kind,
+              "Q and Qout must be (%d, q_heads, %d) %s" % (T, cache.dim, kind))
+        _here(Q, Qout)
+        q, qo, heads, qs, qos = Q.data_ptr(), Qout.data_ptr(), Q.shape[1], Q.stride(), Qout.stride()
+    ks, vs = K.stride(), V.stride()
+    st = lib().dg_kv_append(desc and desc.handle, cache.ref, 2 if kind is torch.float16 else 1, q, qs[0], qs[1], qo,
+                            qos[0], qos[1], heads, K.data_ptr(), ks[0], ks[1], V.data_ptr(), vs[0], vs[1], p, c, s,
+                            rows, slots.data_ptr(), T, _stream(stream))
+    if st != DG_OK:
+        raise DgError(st, "dg_kv_append")
+    return cache
+
+
+def _check_paged(desc, Q, cache, cu_q, kv_len, page_table, O):
+    import torch
+    _check_heads(Q, cache.dim, "Q")
+    _check_heads(O, cache.dim, "O")
+    out = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[desc.fields["out"]]
+    _need(Q.dtype is cache.in_type, "Q must be %s" % cache.in_type)
+    _need(O.shape == Q.shape and O.dtype is out, "O must have Q's shape and the descriptor's output type")
+    _need(Q.shape[1] % cache.heads == 0, "Q's heads must be a multiple of the cache's")
+    B = kv_len.shape[0] if kv_len.dim() == 1 else -1
+    i32 = torch.int32
+    _need(B >= 0 and kv_len.dtype is i32 and cu_q.dtype is i32 and page_table.dtype is i32 and
+          tuple(cu_q.shape) == (B + 1,) and page_table.dim() == 2 and page_table.shape[0] == B and
+          cu_q.is_contiguous() and kv_len.is_contiguous() and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
+          "cu_q (B + 1), kv_len (B) and page_table (B, width) must be int32 with whole rows")
+
+
+def dg_attention_paged_bytes(desc: AttnDesc, cache: KvCache, rows, q_heads, batch, max_q, max_kv) -> int:
+    """Bytes of the workspace that such a dg_attention_paged call takes (0: none)."""
+    return int(lib().dg_attention_paged_bytes(desc.handle, cache.ref, rows, q_heads, batch, max_q, max_kv))
+
+
+def dg_attention_paged(desc: AttnDesc, Q, cache: KvCache, cu_q, kv_len, page_table, O, qk_scale, max_q, max_kv,
+                       workspace=None, stream=None):
+    """O = attention of a ragged batch of new tokens over the paged cache, in the
+    descriptor's order.  Q (rows, q_heads, dim): sequence b's new tokens are rows
+    cu_q[b] .. cu_q[b + 1] - 1, the last of its kv_len[b] keys (causal), which
+    lie in the pages page_table[b, 0], page_table[b, 1], ...  O like Q, of the
+    descriptor's output type; rows outside every sequence are left as they are.
+    max_q and max_kv: at least the most new tokens and keys of any sequence.
+    workspace: a contiguous uint8 tensor of dg_attention_paged_bytes, which a call that is
+    captured into a graph needs to have its spans walked side by side; the bits
+    are the same without."""
+    if _tensor is None:
+        _bind_torch()
+    key = (Q.dtype, O.dtype, cu_q.dtype, kv_len.dtype, page_table.dtype)
+    qs, os_, ts = Q.shape, O.shape, page_table.shape
+    qt, ot = Q.stride(), O.stride()
+    # the usual call in one expression; anything else is named in _check_paged
+    if not (key in _paged_types.get((cache.kind, desc.fields["out"]), ()) and len(qs) == 3 and os_ == qs
+            and qs[2] == cache.dim and qt[2] == 1 and ot[2] == 1 and qs[1] % cache.heads == 0
+            and kv_len.dim() == 1 and cu_q.dim() == 1 and len(ts) == 2 and ts[0] == kv_len.shape[0]
+            and cu_q.shape[0] == ts[0] + 1 and page_table.is_contiguous() and cu_q.is_contiguous()
+            and kv_len.is_contiguous()):
+        _check_paged(desc, Q, cache, cu_q, kv_len, page_table, O)
+        _paged_types.setdefault((cache.kind, desc.fields["out"]), set()).add(key)
+    _need(cache.device == _get_device(), "the cache must be on the current GPU")
+    _here(Q, O, cu_q, kv_len, page_table)
+    ws, wb = None, 0
+    if workspace is not None:
+        _need(workspace.element_size() == 1 and workspace.is_contiguous(), "workspace must be contiguous bytes")
+        _here(workspace)
+        ws, wb = workspace.data_ptr(), workspace.numel()
+    st = lib().dg_attention_paged(desc.handle, 2 if cache.kind == 2 else 1, Q.data_ptr(), qt[0], qt[1], cache.ref,
+                                  cu_q.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), ts[1],
+                                  page_table.stride(0), O.data_ptr(), ot[0], ot[1], qs[0], qs[1], ts[0], max_q,
+                                  max_kv, qk_scale, ws, wb, _stream(stream))
+    if st != DG_OK:
+        raise DgError(st, "dg_attention_paged")
+    return O
+
+
+_paged_types = {}   # the tensors' types that a (cache type, output type) was called with and _check_paged took
+
+
 def exported_symbols():
     """Names of the entry points include/dg.h declares."""
     return ["dg_desc_create", "dg_desc_destroy", "dg_desc_signature", "dg_gemm", "dg_gemm_noalloc",
             "dg_gemm_knobs", "dg_rowsum", "dg_rmsnorm", "dg_softmax", "dg_layernorm", "dg_gemm_colsum", "dg_strerror",
             "dg_version", "dg_attn_desc_create", "dg_attn_desc_destroy", "dg_attention",
             "dg_packed_b_bytes", "dg_pack_b", "dg_gemm_packed", "dg_gemm_packed_knobs", "dg_packed_b8_bytes",
-            "dg_pack_b8"]
+            "dg_pack_b8", "dg_rope_desc_create", "dg_rope_desc_destroy", "dg_rope", "dg_kv_append",
+            "dg_attention_paged", "dg_attention_paged_bytes"]
