@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdg.so")
 SOURCES = ["dg_api.cpp", "dg_gemm.hip", "dg_gemm_odd.hip", "dg_gemm_ring.hip", "dg_gemm_ring_tiles.hip", "dg_gemm_ring_f8.hip", "dg_panel.hip", "dg_rowsum.hip", "dg_rownorm.hip", "dg_rownorm_strided.hip",
-           "dg_attn.hip", "dg_attn_split.hip", "dg_attn_paged.hip", "dg_rope.hip"]
+           "dg_attn.hip", "dg_attn_split.hip", "dg_attn_paged.hip", "dg_attn_paged_few.hip", "dg_rope.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # -ffp-contract=off: no multiply-add is fused unless the source spells it out.

@@ -1,0 +1,201 @@
+// dg_attn_paged_few.hip -- paged attention (dg_attn_paged.h) for sequences of at
+// most 16 rows per key head: a decoding step, a few drafted tokens.
+//
+// Bound: HBM, each key and value read once, so what counts is the bytes in
+// flight.  One wave per workgroup takes one span of one key head and needs no
+// barrier; its K rows go straight from memory into registers in the score
+// instruction's operand layout, one block ahead and one more on the way; its V
+// rows, which have to be transposed, into LDS (16-bit elements directly, e4m3
+// through registers, widened), a block ahead.  So four (e4m3: eight) waves
+// fit a CU, each with a block of K and V in flight.
+#include "dg_attn_paged.h"
+
+namespace dg {
+
+template <int D, int KT, bool INST>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KT == 2 && D == 64 ? 2 : 1))) void
+attn_paged_few(PagedArgs a) {
+  typedef PagedTile<D, KT, 16, INST, false> Tile;
+  constexpr bool F16 = KT == 1, E8 = KT == 2;
+  constexpr int W = Tile::W, DC = Tile::DC, QKS = Tile::QKS, ND = Tile::ND, NQ = Tile::NQ, NT = Tile::NT;
+  constexpr int MC = E8 ? D / 16 : DC;                     // 16-byte pieces of a row in the cache
+  constexpr int NLD = W * MC / 64;                         // loads of a V block, 1 KB each
+  typedef std::conditional_t<E8, u32x2, shortx8> k_t;      // 8 elements of a K row
+  __shared__ __attribute__((aligned(1024))) uint16_t V0[W * D];
+  __shared__ __attribute__((aligned(1024))) uint16_t V1[E8 ? 8 : W * D];
+  __shared__ int64_t where[4][W];
+
+  const int kvh = blockIdx.x % a.Hkv, span = blockIdx.y, bat = blockIdx.z;
+  const Seq sq = sequence(a, bat);
+  const int nrow = rows_of(a, sq);
+  if (nrow <= a.row_lo || nrow > a.row_hi || nrow > 16) return;
+
+  // The walk for the rows from .. to - 1 (see attn_paged).
+  auto walk = [&](int from, int to) {
+    from = __builtin_amdgcn_readfirstlane(from);       // uniform, which the loop around hides
+    to = __builtin_amdgcn_readfirstlane(to);
+    const int end = visible(a, sq, (to - 1) / a.g);    // keys that some of the rows see
+    const int vis_first = visible(a, sq, from / a.g);  // and that all see
+    const int nb = (end + W - 1) / W;
+    const int b0 = a.rec ? span * a.span_blocks : 0;
+    const int b1 = a.rec && b0 + a.span_blocks < nb ? b0 + a.span_blocks : nb;
+    if (span > 0 && b0 >= nb) return true;
+
+    int lane = threadIdx.x;
+    asm volatile("" : "+v"(lane));                      // (its addresses are worked out per walk: registers)
+    lane &= 63;
+    const int li = lane & 15, G = lane >> 4;
+    // lane j finds where row j of a block lies
+    const char* Kb = (const char*)a.K + (int64_t)kvh * a.head_stride;
+    const char* Vb = (const char*)a.V + (int64_t)kvh * a.head_stride;
+    const Rows rows{a.page_table + (int64_t)bat * a.table_stride, b1, end};
+    auto ask = [&](int b) { return rows.ask(a, b, W * b + lane); };
+    auto locate = [&](int b, int page) {
+      where[b & 3][lane] = rows.locate(a, b, W * b + lane, page);
+      asm volatile("" ::: "memory");             // other lanes read it
+    };
+    int pg0 = 0, pg1 = 0, page = 0;
+    if (b0 < b1) {
+      pg0 = ask(b0);
+      pg1 = ask(b0 + 1);
+      page = ask(b0 + 2);
+    }
+
+    const int r = li;
+    const bool valid = r >= from && r < to;
+    const int tok = valid ? r / a.g : 0, head = kvh * a.g + (valid ? r % a.g : 0);
+    const int vis = valid ? visible(a, sq, tok) : end;
+    shortx8 qf[QKS];
+    const uint16_t* Qr = a.Q + (int64_t)(sq.q0 + tok) * a.q_token + head * a.q_head;
+#pragma unroll
+    for (int k = 0; k < QKS; ++k)
+      qf[k] = *(const shortx8*)&Qr[32 * k + 8 * G];   // (rows that are not there: the first one's)
+
+    const int kmap = key_of_row<16>(li);
+    int vad[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) vad[dt] = Tile::v_place(lane, dt);
+
+    Tile t;
+    t.start();
+    k_t kA[NQ], kB[NQ];
+    u32x4 vr[E8 ? NLD : 1];
+    auto fetch_k = [&](k_t* kk, int b) {
+      if (b >= b1) return;
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        glb_bytes p = row_at(Kb, where[b & 3][kmap + Tile::tile_key(x)]) + G * sizeof(k_t);
+#pragma unroll
+        for (int k = 0; k < QKS; ++k) kk[QKS * x + k] = *(const __attribute__((address_space(1))) k_t*)(p + 4 * k * sizeof(k_t));
+      }
+    };
+    auto fetch_v = [&](lds_u16 dst, int b) {
+      if (b >= b1) return;
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        const unsigned q = 64 * i + lane, row = q / MC;
+        glb_bytes p = row_at(Vb, where[b & 3][row]);
+        if constexpr (E8) vr[i] = *(const __attribute__((address_space(1))) u32x4*)(p + 16 * (q % MC));
+        else
+          __builtin_amdgcn_global_load_lds((glb_void)(p + 16 * ((q % MC) ^ v_swz<16, DC>(row))),
+                                           (lds_void)(dst + 512 * i), 16, 0, 0);
+      }
+    };
+    auto stash_v = [&]() {
+      if constexpr (E8) {
+#pragma unroll
+        for (int i = 0; i < NLD; ++i) {
+          const unsigned q = 64 * i + lane, row = q / MC, c = 2 * (q % MC);
+          const u32x4 x = vr[i];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            *(u32x4*)&V0[8 * (row * DC + ((c + h) ^ v_swz<16, DC>(row)))] =
+                u32x4{e4m3x2_bf16x2<false>(x[2 * h]), e4m3x2_bf16x2<true>(x[2 * h]),
+                      e4m3x2_bf16x2<false>(x[2 * h + 1]), e4m3x2_bf16x2<true>(x[2 * h + 1])};
+        }
+      }
+    };
+    auto score = [&](const k_t* kk, int u) {
+      if constexpr (E8) {
+        const u32x4 w = {e4m3x2_bf16x2<false>(kk[u][0]), e4m3x2_bf16x2<true>(kk[u][0]), e4m3x2_bf16x2<false>(kk[u][1]),
+                         e4m3x2_bf16x2<true>(kk[u][1])};
+        t.score(u, __builtin_bit_cast(shortx8, w), qf[u % QKS]);
+      } else t.score(u, kk[u], qf[u % QKS]);
+    };
+    // block b: its K rows were in kc, the next block's are in kn
+    auto step = [&](int b, lds_u16 Vc, lds_u16 Vn, k_t* kc, const k_t* kn) {
+      if constexpr (E8) stash_v();
+      else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+      asm volatile("" ::: "memory");
+      locate(b + 2, page);
+      fetch_k(kc, b + 2);
+      fetch_v(Vn, b + 1);
+      page = ask(b + 3);
+      if (vis_first < (W * b + W < end ? W * b + W : end)) {
+        // keys that only some of the rows see: no infinity or NaN among their values?
+        uint32_t bad = 0;
+#pragma unroll 4
+        for (int i = lane; i < W * DC; i += 64) bad |= not_finite<F16>(*(const lds_x4*)&Vc[8 * i]);
+        if (__builtin_amdgcn_ballot_w64(bad != 0)) return false;
+      }
+      t.block(a, W * b, vis, vis_first, G, Vc, vad, [&](int u) { score(kn, u); });
+      return true;
+    };
+    bool whole = true;
+    if (b0 < b1) {
+      locate(b0, pg0);
+      fetch_k(kA, b0);
+      fetch_v((lds_u16)V0, b0);
+      locate(b0 + 1, pg1);
+      fetch_k(kB, b0 + 1);
+#pragma unroll
+      for (int u = 0; u < NQ; ++u) score(kA, u);
+      for (int b = b0; whole && b < b1; b += 2) {
+        whole = step(b, (lds_u16)V0, E8 ? (lds_u16)V0 : (lds_u16)V1, kA, kB);
+        if (whole && b + 1 < b1) whole = step(b + 1, E8 ? (lds_u16)V0 : (lds_u16)V1, (lds_u16)V0, kB, kA);
+      }
+      if (!whole) {
+        if constexpr (!E8) __builtin_amdgcn_s_waitcnt(vmcnt_only(0));   // before the buffers' next use
+        return false;
+      }
+    }
+    if (valid) leave(a, t, sq, bat, kvh, r, tok, head, vis, span, W * b0, G);
+    return true;
+  };
+
+  // rows of several tokens, whole or, where they hold such values, a token at a time
+  for (int from = 0, to = nrow;;) {
+    if (!walk(from, to)) {
+      to = (from / a.g + 1) * a.g < nrow ? (from / a.g + 1) * a.g : nrow;
+      continue;
+    }
+    if (to == nrow) break;
+    from = to;
+    to = to + a.g < nrow ? to + a.g : nrow;
+  }
+}
+
+namespace {
+
+template <int D, int KT, bool INST>
+hipError_t launch_few(const PagedArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)a.Hkv, (unsigned)(a.rec ? a.nspan : 1), (unsigned)a.B);
+  hipLaunchKernelGGL((attn_paged_few<D, KT, INST>), grid, dim3(64), 0, st, a);
+  return hipGetLastError();
+}
+
+template <int D, bool INST>
+hipError_t launch_few_type(const PagedArgs& a, hipStream_t st) {
+  if (a.kv_dtype == DG_E4M3) return launch_few<D, 2, INST>(a, st);
+  if (a.kv_dtype == DG_F16) return launch_few<D, 1, INST>(a, st);
+  return launch_few<D, 0, INST>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_attention_paged_few(const PagedArgs& a, hipStream_t st) {
+  if (a.dim == 64) return a.inst ? launch_few_type<64, true>(a, st) : launch_few_type<64, false>(a, st);
+  return a.inst ? launch_few_type<128, true>(a, st) : launch_few_type<128, false>(a, st);
+}
+
+}  // namespace dg

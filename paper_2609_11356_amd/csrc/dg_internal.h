@@ -121,6 +121,7 @@ struct PagedArgs {
 
 // nw waves of rw rows per workgroup: (1, 16), (4, 16) or (4, 32)
 hipError_t launch_attention_paged(const PagedArgs& a, int nw, int rw, hipStream_t s);
+hipError_t launch_attention_paged_few(const PagedArgs& a, hipStream_t s);   // at most 16 rows per key head, one span per walk
 hipError_t launch_attention_paged_join(const PagedArgs& a, hipStream_t s);
 
 // Rotary positions and the cache append (dg_rope.hip).
