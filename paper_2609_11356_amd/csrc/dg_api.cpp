@@ -1483,9 +1483,18 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
   if (most > 16) {
     PagedLaunch& l = p.l[p.n++];
     l = PagedLaunch{4, 16, p.n > 1 ? 16 : 0, INT32_MAX, 0, false, 0};
-    // workgroups of 64 rows fill the chip's 512 places, or their spans do
-    const int64_t tiles = std::min((rows * g + 63) / 64 + batch, (most + 63) / 64 * batch);
-    l.split = spans && tiles * c->heads < 512;
+    const auto groups = [&](int64_t r) {   // workgroups of r rows
+      return std::min((rows * g + r - 1) / r + batch / 2, (most + r - 1) / r * batch) * c->heads;
+    };
+    // few rows: 16 to a wave.  One workgroup for all the spans of a tile where
+    // the tiles fill the chip, or nearly; else the spans apart.
+    if (most <= 64) l.split = spans && groups(64) < 512;
+    else {
+      l.rw = 32;
+      if (c->dim == 64) l.split = spans && groups(128) < 400;
+      else if (groups(256) >= 200) l.nw = 8;
+      else l.split = spans && groups(128) < 200;
+    }
     l.records = (size_t)rows * q_heads;
   }
   for (int i = 0; i < p.n; ++i) {
@@ -1532,6 +1541,10 @@ dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void*
   if (table_width < 0 || !stride_ok(table_stride) || (batch > 1 && table_stride < table_width)) return DG_ERR_SHAPE;
   if (table_width > PAGED_SIZES / c->page) return DG_ERR_SHAPE;
   if (!stride_ok(q_token) || !stride_ok(q_head) || !stride_ok(o_token) || !stride_ok(o_head)) return DG_ERR_SHAPE;
+  // offsets within a page, and a page's, in 31 bits
+  const int64_t bytes = c->dtype == DG_E4M3 ? 1 : 2;
+  if (c->page_stride * bytes > INT32_MAX || (c->page > 1 && c->token_stride * bytes > INT32_MAX / (c->page - 1)))
+    return DG_ERR_SHAPE;
   // the instruction's form takes the largest score times the scale as the largest product
   if (d->p.exp2 == DG_EXP2_INST && !(qk_scale > 0.f)) return DG_ERR_INVALID;
   if (rows == 0 || q_heads == 0 || batch == 0) return DG_OK;
@@ -1572,8 +1585,9 @@ dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void*
   // / page) + 1 the product is off by less than 2^(31 + s) / page, as mul * page
   // exceeds 2^(31 + s) by at most page <= 2^s
   while (((int64_t)1 << a.page_shift) < c->page) ++a.page_shift;
-  a.page_shift += 31;
-  a.page_mul = (uint32_t)((((uint64_t)1 << a.page_shift) / (uint64_t)c->page) + 1);
+  a.page_mul = (uint32_t)((((uint64_t)1 << (31 + a.page_shift)) / (uint64_t)c->page) + 1);
+  a.page_step = (int32_t)(64 / c->page);
+  a.page_rest = (int32_t)(64 % c->page);
   a.max_q = (int32_t)max_q;
   a.span_blocks = d->p.split_keys / 64;
   a.causal = d->p.causal;

@@ -117,38 +117,54 @@ typedef __attribute__((address_space(3))) uint16_t* lds_u16;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) shortx8 lds_s8;
 typedef __attribute__((address_space(3))) u32x4 lds_x4;
+typedef __attribute__((address_space(3))) floatx4 lds_f4;
 
-// Where the row at byte offset w of a cache begins (-1, -2: the constant rows).
-__device__ __forceinline__ glb_bytes row_at(const char* base, int64_t w) {
-  const int64_t fill = (int64_t)(const char*)kFill.w[0] - (w == -2 ? -256 : 0);
-  return (glb_bytes)(w >= 0 ? (int64_t)base + w : fill);
-}
+// A lane's row of the walk's blocks in the cache.  Its place moves on by 64 keys
+// with every block; the row's addresses in K and V, or of the constant row that
+// stands for it, go into a ring in LDS, from where the lanes that load the row
+// take them.  All by selects: registers that the compiler moves about at the join
+// of a divergent branch would lose the lanes that were not in it.
+struct RowAddress {
+  int64_t k, v;
+};
+typedef __attribute__((address_space(3))) RowAddress* lds_rows;
+struct Row {
+  int key, index, rest;          // the key of the next block to ask for; its page in the table, its place there
+  int page, asked;               // the answer, and the place there of the key it is for (-1: past the end)
 
-// The keys of one walk's sequence in the cache, for a lane's rows.  All by
-// selects: registers that the compiler moves about at the join of a divergent
-// branch would lose the lanes that were not in it.
-struct Rows {
-  const int32_t* table;
-  int b1, end;                   // blocks and keys of the walk
-  __device__ __forceinline__ int page_of(const PagedArgs& a, int key) const {
-    return (int)(((uint64_t)(uint32_t)key * a.page_mul) >> a.page_shift);
+  __device__ __forceinline__ void start(const PagedArgs& a, int first) {
+    key = first;
+    index = (int)(__umulhi(2u * (uint32_t)first, a.page_mul) >> a.page_shift);
+    rest = first - index * a.page_size;
   }
-  // the page number of key's row in block b (any page's past the walk's end)
-  __device__ __forceinline__ int ask(const PagedArgs& a, int b, int key) const {
-    return table[b < b1 && key < end ? page_of(a, key) : 0];
+  // asks for the next block's page number (keys from `end` on: any page's)
+  __device__ __forceinline__ void ask(const PagedArgs& a, const int32_t* table, int end) {
+    const bool in = key < end;
+    page = table[in ? index : 0];
+    asked = in ? rest : -1;
+    key += 64;
+    index += a.page_step;
+    rest += a.page_rest;
+    const bool over = rest >= a.page_size;
+    rest -= over ? a.page_size : 0;
+    index += over ? 1 : 0;
   }
-  // its byte offset in K and V, or which constant row stands for it
-  __device__ __forceinline__ int64_t locate(const PagedArgs& a, int b, int key, int page) const {
-    const int64_t w = (int64_t)page * a.page_stride + (int64_t)(key - page_of(a, key) * a.page_size) * a.token_stride;
-    return b < b1 && key < end ? ((uint32_t)page < (uint32_t)a.pages ? w : -2) : -1;
+  // the answer as addresses; offsets within a page fit 31 bits
+  __device__ __forceinline__ RowAddress locate(const PagedArgs& a, int64_t kb, int64_t vb) const {
+    const bool there = (uint32_t)page < (uint32_t)a.pages;
+    const uint64_t w = (uint64_t)(uint32_t)page * (uint32_t)a.page_stride + (uint32_t)asked * (uint32_t)a.token_stride;
+    const int64_t fill = (int64_t)(const char*)kFill.w[0], none = fill + 256;
+    const bool in = asked >= 0;
+    return RowAddress{in ? (there ? kb + (int64_t)w : none) : fill, in ? (there ? vb + (int64_t)w : none) : fill};
   }
 };
 
 // The state of a wave's RW rows over transposed score tiles, as in attn_fwd_t
 // (dg_attn.hip): a lane owns one row (lane % RW), G = lane / RW names its share of
 // the keys, P~ stays in registers.  KT: the cache's elements, 0 bf16, 1 binary16,
-// 2 e4m3 (widened exactly to bf16).  JOINS: the wave walks more than one span.
-template <int D, int KT, int RW, bool INST, bool JOINS>
+// 2 e4m3 (widened exactly to bf16).  JOINS: the wave walks more than one span; then
+// TL of the registers of a lane's joined output, which is touched once a span, are in LDS.
+template <int D, int KT, int RW, bool INST, bool JOINS, int TL = 0>
 struct PagedTile {
   static constexpr bool F16 = KT == 1;
   static constexpr int W = 64, DC = D / 8, KS = RW == 32 ? 16 : 32;   // keys per block; chunks of a row; keys per P V step
@@ -159,7 +175,10 @@ struct PagedTile {
   typedef std::conditional_t<RW == 32, floatx16, floatx4> tile_t;
 
   float m, l, M, L;              // the span's and the row's maximum and denominator
-  tile_t O[ND], T[JOINS ? ND : 1], Sn[NT];   // their output rows (transposed); the next block's scores
+  tile_t O[ND], Sn[NT];          // the span's output rows (transposed); the next block's scores
+  static constexpr int TV = JOINS ? (ND * TR - TL) / 4 : 0;
+  floatx4 T[TV ? TV : 1];        // the row's, four columns each: the last TV, and before them
+  lds_f4* tl;                    // TL / 4 in LDS, 64 places apart
 
   // first key of score tile t relative to the lane's kmap (key_of_row)
   static constexpr __device__ int tile_key(int t) { return RW == 32 ? 32 * t : 32 * (t >> 1) + 4 * (t & 1); }
@@ -183,12 +202,22 @@ struct PagedTile {
   }
   __device__ __forceinline__ void start() {
     start_span();
-    if constexpr (JOINS) {
-      M = m;
-      L = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) T[dt] = O[dt];
-    }
+    M = m;
+    L = 0.f;
+  }
+
+  // the row's output, columns column(dt, c) + 4 G + 0..3
+  __device__ __forceinline__ floatx4 joined(int dt, int c) const {
+    const int i = dt * (TR / 4) + c;
+    return i < TL / 4 ? tl[64 * i] : T[i < TL / 4 ? 0 : i - TL / 4];
+  }
+  __device__ __forceinline__ void set_joined(int dt, int c, floatx4 y) {
+    const int i = dt * (TR / 4) + c;
+    if (i < TL / 4) tl[64 * i] = y;
+    else T[i < TL / 4 ? 0 : i - TL / 4] = y;
+  }
+  __device__ __forceinline__ floatx4 span_part(int dt, int c) const {
+    return floatx4{O[dt][4 * c], O[dt][4 * c + 1], O[dt][4 * c + 2], O[dt][4 * c + 3]};
   }
 
   // score instruction u of a block: head-dimension step u % QKS of tile u / QKS
@@ -310,15 +339,25 @@ struct PagedTile {
       M = m;
       L = l;
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) T[dt] = O[dt];
-    } else if (vis > first) {
-      float ea, eb;
-      join<INST>(M, m, ea, eb);
-      L = __builtin_fmaf(eb, l, ea * L);
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int c = 0; c < TR / 4; ++c) set_joined(dt, c, span_part(dt, c));
+    } else {
+      // (selects, no branch: a row that does not see the span keeps its state)
+      const bool sees = vis > first;
+      float Mn = M, ea, eb;
+      join<INST>(Mn, m, ea, eb);
+      M = sees ? Mn : M;
+      L = sees ? __builtin_fmaf(eb, l, ea * L) : L;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int i = 0; i < TR; ++i) T[dt][i] = __builtin_fmaf(eb, O[dt][i], ea * T[dt][i]);
+        for (int c = 0; c < TR / 4; ++c) {
+          floatx4 y = joined(dt, c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = sees ? __builtin_fmaf(eb, O[dt][4 * c + e], ea * y[e]) : y[e];
+          set_joined(dt, c, y);
+        }
     }
     start_span();
   }
@@ -339,21 +378,17 @@ struct PagedTile {
   }
   // The answer at element `at` of O; a row that sees nothing is zero.
   __device__ __forceinline__ void answer(const PagedArgs& a, int64_t at, int vis, int G) const {
-    const tile_t* rows = O;
-    float sum = l;
-    if constexpr (JOINS) {
-      rows = T;
-      sum = L;
-    }
+    const float sum = JOINS ? L : l;
     const float rcp = 1.0f / sum;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
       for (int c = 0; c < TR / 4; ++c) {
+        const floatx4 o = JOINS ? joined(dt, c) : span_part(dt, c);
         float y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float x = a.final_recip ? rows[dt][4 * c + e] * rcp : rows[dt][4 * c + e] / sum;
+          const float x = a.final_recip ? o[e] * rcp : o[e] / sum;
           y[e] = vis > 0 ? x * a.v_scale : 0.f;
         }
         store4(a, at + column(dt, c) + 4 * G, y);

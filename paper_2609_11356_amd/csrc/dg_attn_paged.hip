@@ -8,10 +8,10 @@ namespace dg {
 // One workgroup: NW waves of RW rows of one key head of one sequence, over all
 // of the keys that they see (a.rec null) or over one span of them, K a block
 // ahead of V in LDS.
-template <int D, int KT, int NW, int RW, bool INST, bool JOINS>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 1 ? 1 : 2))) void
+template <int D, int KT, int NW, int RW, bool INST, bool JOINS, int TL>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 4 && TL ? 1 : 2))) void
 attn_paged(PagedArgs a) {
-  typedef PagedTile<D, KT, RW, INST, JOINS> Tile;
+  typedef PagedTile<D, KT, RW, INST, JOINS, TL> Tile;
   constexpr bool F16 = KT == 1, E8 = KT == 2;
   constexpr int W = Tile::W, DC = Tile::DC, QKS = Tile::QKS, ND = Tile::ND, NQ = Tile::NQ;
   constexpr int MC = E8 ? D / 16 : DC;                     // 16-byte pieces of a row in the cache
@@ -22,8 +22,9 @@ attn_paged(PagedArgs a) {
   __shared__ __attribute__((aligned(1024))) uint16_t K1[W * D];
   __shared__ __attribute__((aligned(1024))) uint16_t V1[W * D];
   constexpr int RPW = W / NW;                              // rows of a block that a wave loads
-  __shared__ int64_t where[4][W];
+  __shared__ RowAddress where[4][W];
   __shared__ int spoilt[2];
+  __shared__ __attribute__((aligned(16))) float joined[JOINS && TL ? NW * 64 * TL : 4];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % a.Hkv, span = blockIdx.y, bat = blockIdx.z;
@@ -73,21 +74,20 @@ attn_paged(PagedArgs a) {
     qf[k] = *(const shortx8*)&Qr[Tile::KS * k + 8 * G];   // (rows that are not there: the first one's)
 
   Tile t;
+  t.tl = (lds_f4*)joined + (JOINS && TL ? 64 * (TL / 4) * wave + lane : 0);
   t.start();
 
-  // Where a block's rows lie.  A wave loads RPW rows of a block; lane j % RPW
-  // finds row j's page (asked for a block before its use) and leaves the row's
-  // byte offset in K and V, or which constant row stands for it (-1, -2), in
-  // the wave's ring of four blocks in LDS.
-  const char* Kb = (const char*)a.K + (int64_t)kvh * a.head_stride;
-  const char* Vb = (const char*)a.V + (int64_t)kvh * a.head_stride;
-  const Rows rows{a.page_table + (int64_t)bat * a.table_stride, b1, end};
+  // a wave loads RPW rows of a block; lane j finds row j % RPW (asked for a block
+  // before its use; lanes of one row write the same)
+  const int64_t Kb = (int64_t)a.K + (int64_t)kvh * a.head_stride, Vb = (int64_t)a.V + (int64_t)kvh * a.head_stride;
+  const int32_t* table = a.page_table + (int64_t)bat * a.table_stride;
+  const int last = end < W * b1 ? end : W * b1;        // the walk's last key, and one
   const int own_row = RPW * wave + (lane & (RPW - 1));
-  int page = 0;
-  auto ask = [&](int b) { page = rows.ask(a, b, W * b + own_row); };
+  Row row;
+  row.start(a, W * b0 + own_row);
+  auto ask = [&]() { row.ask(a, table, last); };
   auto locate = [&](int b) {
-    // (lanes of one row write the same)
-    where[b & 3][own_row] = rows.locate(a, b, W * b + own_row, page);
+    where[b & 3][own_row] = row.locate(a, Kb, Vb);
     asm volatile("" ::: "memory");               // other lanes of the wave read it
   };
   // straight into LDS (the lane fetches the piece that belongs at its place), or
@@ -99,10 +99,10 @@ attn_paged(PagedArgs a) {
     for (int i = 0; i < NLD; ++i) {
       const unsigned q = 64 * (NLD * wave + i) + lane, t = q / MC;
       if constexpr (E8) {
-        (v ? vr : kr)[i] = *(const __attribute__((address_space(1))) u32x4*)(row_at(v ? Vb : Kb, where[b & 3][t]) + 16 * (q % MC));
+        (v ? vr : kr)[i] = *(const __attribute__((address_space(1))) u32x4*)((glb_bytes)(v ? where[b & 3][t].v : where[b & 3][t].k) + 16 * (q % MC));
       } else {
         const int c = (q % MC) ^ (v ? v_swz<RW, DC>(t) : k_swz<RW, DC>(t));
-        __builtin_amdgcn_global_load_lds((glb_void)(row_at(v ? Vb : Kb, where[b & 3][t]) + 16 * c),
+        __builtin_amdgcn_global_load_lds((glb_void)((glb_bytes)(v ? where[b & 3][t].v : where[b & 3][t].k) + 16 * c),
                                          (lds_void)(dst + 512 * (NLD * wave + i)), 16, 0, 0);
       }
     }
@@ -163,12 +163,12 @@ attn_paged(PagedArgs a) {
       locate(b + 3);
       fetch(false, Kc, b + 3);
       fetch(true, Vn, b + 2);
-      ask(b + 4);
+      ask();
     } else {
       locate(b + 2);
       fetch(false, Kc, b + 2);
       fetch(true, Vn, b + 1);
-      ask(b + 3);
+      ask();
     }
     t.block(a, W * b, vis, vis_least, G, Vc, vad, [&](int u) { score(Kn, u); });
     if constexpr (JOINS) if (b + 1 - folded == a.span_blocks || b + 1 == b1) {
@@ -180,27 +180,27 @@ attn_paged(PagedArgs a) {
   if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
   bool whole = true;
   if (b0 < b1) {
-    ask(b0);
+    ask();
     locate(b0);
     fetch(false, (lds_u16)K0, b0);
     fetch(true, (lds_u16)V0, b0);
     stash(false, (lds_u16)K0, b0);
     stash(true, (lds_u16)V0, b0);
-    ask(b0 + 1);
+    ask();
     locate(b0 + 1);
     if constexpr (E8) {
       fetch(false, (lds_u16)K1, b0 + 1);
       stash(false, (lds_u16)K1, b0 + 1);
       fetch(true, (lds_u16)V1, b0 + 1);
-      ask(b0 + 2);
+      ask();
       locate(b0 + 2);
       fetch(false, (lds_u16)K0, b0 + 2);
-      ask(b0 + 3);
+      ask();
       turn();
     } else {
       turn();
       fetch(false, (lds_u16)K1, b0 + 1);
-      ask(b0 + 2);
+      ask();
     }
 #pragma unroll
     for (int u = 0; u < NQ; ++u) score((lds_u16)K0, u);
@@ -309,20 +309,29 @@ __global__ __launch_bounds__(64) void attn_paged_join(PagedArgs a) {
 
 namespace {
 
-template <int D, int KT, int NW, int RW, bool INST>
+template <int D, int KT, int NW, int RW, bool INST, bool JOINS, int TL>
 hipError_t launch_one(const PagedArgs& a, hipStream_t st) {
   constexpr int R = NW * RW;
   const int64_t most = (int64_t)a.max_q * a.g;
   const int64_t rows = a.row_hi < most ? a.row_hi : most;
   const dim3 grid((unsigned)((rows + R - 1) / R * a.Hkv), (unsigned)(a.rec ? a.nspan : 1), (unsigned)a.B);
-  if (!a.rec && a.nspan > 1) hipLaunchKernelGGL((attn_paged<D, KT, NW, RW, INST, true>), grid, dim3(64 * NW), 0, st, a);
-  else hipLaunchKernelGGL((attn_paged<D, KT, NW, RW, INST, false>), grid, dim3(64 * NW), 0, st, a);
+  hipLaunchKernelGGL((attn_paged<D, KT, NW, RW, INST, JOINS, TL>), grid, dim3(64 * NW), 0, st, a);
   return hipGetLastError();
 }
 
+// d = 128 with spans to join has no registers for 64 more of output: with eight
+// waves a CU (one workgroup) 44 of them go to LDS, with four all of them.
 template <int D, int KT, bool INST>
 hipError_t launch_tile(const PagedArgs& a, int nw, int rw, hipStream_t st) {
-  return launch_one<D, KT, 4, 16, INST>(a, st);
+  const bool joins = !a.rec && a.nspan > 1;
+  if (rw == 16) {
+    if (joins) return launch_one<D, KT, 4, 16, INST, true, 0>(a, st);
+    return launch_one<D, KT, 4, 16, INST, false, 0>(a, st);
+  }
+  if (!joins) return launch_one<D, KT, 4, 32, INST, false, 0>(a, st);
+  if constexpr (D == 64) return launch_one<D, KT, 4, 32, INST, true, 0>(a, st);
+  else if (nw == 8) return launch_one<D, KT, 8, 32, INST, true, 44>(a, st);
+  else return launch_one<D, KT, 4, 32, INST, true, 64>(a, st);
 }
 
 template <int D, bool INST>

@@ -23,7 +23,7 @@ attn_paged_few(PagedArgs a) {
   typedef std::conditional_t<E8, u32x2, shortx8> k_t;      // 8 elements of a K row
   __shared__ __attribute__((aligned(1024))) uint16_t V0[W * D];
   __shared__ __attribute__((aligned(1024))) uint16_t V1[E8 ? 8 : W * D];
-  __shared__ int64_t where[4][W];
+  __shared__ RowAddress where[4][W];
 
   const int kvh = blockIdx.x % a.Hkv, span = blockIdx.y, bat = blockIdx.z;
   const Seq sq = sequence(a, bat);
@@ -46,19 +46,23 @@ attn_paged_few(PagedArgs a) {
     lane &= 63;
     const int li = lane & 15, G = lane >> 4;
     // lane j finds where row j of a block lies
-    const char* Kb = (const char*)a.K + (int64_t)kvh * a.head_stride;
-    const char* Vb = (const char*)a.V + (int64_t)kvh * a.head_stride;
-    const Rows rows{a.page_table + (int64_t)bat * a.table_stride, b1, end};
-    auto ask = [&](int b) { return rows.ask(a, b, W * b + lane); };
-    auto locate = [&](int b, int page) {
-      where[b & 3][lane] = rows.locate(a, b, W * b + lane, page);
+    const int64_t Kb = (int64_t)a.K + (int64_t)kvh * a.head_stride, Vb = (int64_t)a.V + (int64_t)kvh * a.head_stride;
+    const int32_t* table = a.page_table + (int64_t)bat * a.table_stride;
+    const int last = end < W * b1 ? end : W * b1;      // the walk's last key, and one
+    Row row;
+    row.start(a, W * b0 + lane);
+    auto ask = [&]() { row.ask(a, table, last); };
+    auto locate = [&](int b, const Row& rw) {
+      where[b & 3][lane] = rw.locate(a, Kb, Vb);
       asm volatile("" ::: "memory");             // other lanes read it
     };
-    int pg0 = 0, pg1 = 0, page = 0;
+    Row row0, row1;                              // the first two blocks' answers
     if (b0 < b1) {
-      pg0 = ask(b0);
-      pg1 = ask(b0 + 1);
-      page = ask(b0 + 2);
+      ask();
+      row0 = row;
+      ask();
+      row1 = row;
+      ask();
     }
 
     const int r = li;
@@ -76,15 +80,15 @@ attn_paged_few(PagedArgs a) {
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) vad[dt] = Tile::v_place(lane, dt);
 
-    Tile t;
-    t.start();
+    Tile tile;
+    tile.start();
     k_t kA[NQ], kB[NQ];
     u32x4 vr[E8 ? NLD : 1];
     auto fetch_k = [&](k_t* kk, int b) {
       if (b >= b1) return;
 #pragma unroll
       for (int x = 0; x < NT; ++x) {
-        glb_bytes p = row_at(Kb, where[b & 3][kmap + Tile::tile_key(x)]) + G * sizeof(k_t);
+        glb_bytes p = (glb_bytes)where[b & 3][kmap + Tile::tile_key(x)].k + G * sizeof(k_t);
 #pragma unroll
         for (int k = 0; k < QKS; ++k) kk[QKS * x + k] = *(const __attribute__((address_space(1))) k_t*)(p + 4 * k * sizeof(k_t));
       }
@@ -93,11 +97,11 @@ attn_paged_few(PagedArgs a) {
       if (b >= b1) return;
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
-        const unsigned q = 64 * i + lane, row = q / MC;
-        glb_bytes p = row_at(Vb, where[b & 3][row]);
+        const unsigned q = 64 * i + lane, t = q / MC;
+        glb_bytes p = (glb_bytes)where[b & 3][t].v;
         if constexpr (E8) vr[i] = *(const __attribute__((address_space(1))) u32x4*)(p + 16 * (q % MC));
         else
-          __builtin_amdgcn_global_load_lds((glb_void)(p + 16 * ((q % MC) ^ v_swz<16, DC>(row))),
+          __builtin_amdgcn_global_load_lds((glb_void)(p + 16 * ((q % MC) ^ v_swz<16, DC>(t))),
                                            (lds_void)(dst + 512 * i), 16, 0, 0);
       }
     };
@@ -105,11 +109,11 @@ attn_paged_few(PagedArgs a) {
       if constexpr (E8) {
 #pragma unroll
         for (int i = 0; i < NLD; ++i) {
-          const unsigned q = 64 * i + lane, row = q / MC, c = 2 * (q % MC);
+          const unsigned q = 64 * i + lane, t = q / MC, c = 2 * (q % MC);
           const u32x4 x = vr[i];
 #pragma unroll
           for (int h = 0; h < 2; ++h)
-            *(u32x4*)&V0[8 * (row * DC + ((c + h) ^ v_swz<16, DC>(row)))] =
+            *(u32x4*)&V0[8 * (t * DC + ((c + h) ^ v_swz<16, DC>(t)))] =
                 u32x4{e4m3x2_bf16x2<false>(x[2 * h]), e4m3x2_bf16x2<true>(x[2 * h]),
                       e4m3x2_bf16x2<false>(x[2 * h + 1]), e4m3x2_bf16x2<true>(x[2 * h + 1])};
         }
@@ -119,18 +123,18 @@ attn_paged_few(PagedArgs a) {
       if constexpr (E8) {
         const u32x4 w = {e4m3x2_bf16x2<false>(kk[u][0]), e4m3x2_bf16x2<true>(kk[u][0]), e4m3x2_bf16x2<false>(kk[u][1]),
                          e4m3x2_bf16x2<true>(kk[u][1])};
-        t.score(u, __builtin_bit_cast(shortx8, w), qf[u % QKS]);
-      } else t.score(u, kk[u], qf[u % QKS]);
+        tile.score(u, __builtin_bit_cast(shortx8, w), qf[u % QKS]);
+      } else tile.score(u, kk[u], qf[u % QKS]);
     };
     // block b: its K rows were in kc, the next block's are in kn
     auto step = [&](int b, lds_u16 Vc, lds_u16 Vn, k_t* kc, const k_t* kn) {
       if constexpr (E8) stash_v();
       else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
       asm volatile("" ::: "memory");
-      locate(b + 2, page);
+      locate(b + 2, row);
       fetch_k(kc, b + 2);
       fetch_v(Vn, b + 1);
-      page = ask(b + 3);
+      ask();
       if (vis_first < (W * b + W < end ? W * b + W : end)) {
         // keys that only some of the rows see: no infinity or NaN among their values?
         uint32_t bad = 0;
@@ -138,15 +142,15 @@ attn_paged_few(PagedArgs a) {
         for (int i = lane; i < W * DC; i += 64) bad |= not_finite<F16>(*(const lds_x4*)&Vc[8 * i]);
         if (__builtin_amdgcn_ballot_w64(bad != 0)) return false;
       }
-      t.block(a, W * b, vis, vis_first, G, Vc, vad, [&](int u) { score(kn, u); });
+      tile.block(a, W * b, vis, vis_first, G, Vc, vad, [&](int u) { score(kn, u); });
       return true;
     };
     bool whole = true;
     if (b0 < b1) {
-      locate(b0, pg0);
+      locate(b0, row0);
       fetch_k(kA, b0);
       fetch_v((lds_u16)V0, b0);
-      locate(b0 + 1, pg1);
+      locate(b0 + 1, row1);
       fetch_k(kB, b0 + 1);
 #pragma unroll
       for (int u = 0; u < NQ; ++u) score(kA, u);
@@ -159,7 +163,7 @@ attn_paged_few(PagedArgs a) {
         return false;
       }
     }
-    if (valid) leave(a, t, sq, bat, kvh, r, tok, head, vis, span, W * b0, G);
+    if (valid) leave(a, tile, sq, bat, kvh, r, tok, head, vis, span, W * b0, G);
     return true;
   };
 

@@ -111,7 +111,8 @@ struct PagedArgs {
   float2* rec_ml;                // and their (m, l)
   int32_t dim, rows, B, Hkv, g;
   int32_t pages, page_size, kv_cap;   // kv_cap: keys that the batch's lengths are cut to
-  uint32_t page_mul, page_shift;      // key / page_size = key * page_mul >> page_shift (key < 2^31)
+  uint32_t page_mul, page_shift;      // key / page_size = (2 key * page_mul >> 32) >> page_shift (key < 2^31)
+  int32_t page_step, page_rest;       // 64 / page_size and 64 % page_size
   int32_t max_q, span_blocks, nspan;  // blocks of 64 keys per span; spans of max_kv keys
   int32_t row_lo, row_hi;        // sequences with row_lo < new tokens * g <= row_hi are taken
   int32_t rec_rows;              // records of row r of (sequence, key head): rows reserved for each; 0: by token and head
@@ -119,7 +120,7 @@ struct PagedArgs {
   float qk_scale, v_scale;
 };
 
-// nw waves of rw rows per workgroup: (1, 16), (4, 16) or (4, 32)
+// nw waves of rw rows per workgroup: (1, 16), (4, 16), (4, 32) or (8, 32)
 hipError_t launch_attention_paged(const PagedArgs& a, int nw, int rw, hipStream_t s);
 hipError_t launch_attention_paged_few(const PagedArgs& a, hipStream_t s);   // at most 16 rows per key head, one span per walk
 hipError_t launch_attention_paged_join(const PagedArgs& a, hipStream_t s);

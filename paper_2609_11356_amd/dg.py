@@ -238,13 +238,13 @@ def dg_desc_create(**fields) -> Desc:
 
 # torch's names that every call needs, looked up once (torch is imported when
 # the library is loaded, not with this module)
-_tensor = _raw_stream = _get_device = _bf16 = _f32 = None
+_tensor = _raw_stream = _get_device = _bf16 = _f32 = _i32 = _i64 = None
 
 
 def _bind_torch():
-    global _tensor, _raw_stream, _get_device, _bf16, _f32
+    global _tensor, _raw_stream, _get_device, _bf16, _f32, _i32, _i64
     import torch
-    _bf16, _f32 = torch.bfloat16, torch.float32
+    _bf16, _f32, _i32, _i64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
     _get_device = torch.cuda.current_device
     # the current stream's handle without building a Stream object (0.1 us
     # instead of 3); the public way where this torch does not have it
@@ -283,7 +283,7 @@ def _need(cond, msg):
 
 def _out_dtype(desc):
     import torch
-    return torch.bfloat16 if desc.fields["out"] == "bf16" else torch.float32
+    return {"bf16": torch.bfloat16, "f16": torch.float16}.get(desc.fields["out"], torch.float32)
 
 
 def _on_device(*ts):
@@ -685,6 +685,7 @@ class RopeDesc:
             raise DgError(st, "dg_rope_desc_create")
         self.handle = h
         self.dim, self.rotary, self.pairing, self.axes, self.n_axes = int(dim), int(rotary), pairing, axes, p.n_axes
+        self.half = self.rotary // 2
 
     def __del__(self):
         h = getattr(self, "handle", None)
@@ -738,23 +739,40 @@ def _check_heads(X, dim, name):
           "%s must be (tokens, heads, %d) with whole heads" % (name, dim))
 
 
+def _check_rope(desc, X, pos, cos, sin, Y):
+    _check_heads(X, desc.dim, "X")
+    _check_heads(Y, desc.dim, "Y")
+    _need(Y.shape == X.shape and Y.dtype is X.dtype, "Y must have X's shape and dtype")
+    _check_tables(desc, pos, cos, sin, X.shape[0])
+    _here(X, Y)
+    kind = _type_of(X)
+    _need(kind <= 2, "X must be bf16, float16 or fp32")
+    return kind
+
+
 def dg_rope(desc: RopeDesc, X, pos, cos, sin, Y, inverse=False, stream=None):
     """Y = X turned by its tokens' positions (inverse: turned back, which is the
     gradient of X given that of Y).  X and Y (T, H, dim) bf16, float16 or
     fp32, the heads contiguous, at any token and head strides; Y may be X.
     pos (n_axes, T) (or (T,)) int32 rows into the fp32 tables cos and sin (rows,
     rotary / 2)."""
-    _check_heads(X, desc.dim, "X")
-    _check_heads(Y, desc.dim, "Y")
-    _need(Y.shape == X.shape and Y.dtype is X.dtype, "Y must have X's shape and dtype")
-    T, H, _ = X.shape
-    rows = _check_tables(desc, pos, cos, sin, T)
-    _here(X, Y)
-    kind = _type_of(X)
-    _need(kind <= 2, "X must be bf16, float16 or fp32")
+    if _tensor is None:
+        _bind_torch()
+    # the usual call in one expression; anything else is named below
+    shape, table, kind = X.shape, cos.shape, X.dtype
+    device = X.get_device()
     xs, ys = X.stride(), Y.stride()
-    st = lib().dg_rope(desc.handle, kind, X.data_ptr(), xs[0], xs[1], Y.data_ptr(), ys[0], ys[1], pos.data_ptr(),
-                       cos.data_ptr(), sin.data_ptr(), rows, T, H, 1 if inverse else 0, _stream(stream))
+    number = _elements.get(kind)
+    if not (number is not None and number <= 2 and len(shape) == 3 and Y.shape == shape and Y.dtype is kind
+            and shape[2] == desc.dim and xs[2] == 1 and ys[2] == 1 and table == sin.shape
+            and len(table) == 2 and table[1] == desc.half and pos.shape == (desc.n_axes, shape[0])
+            and cos.dtype is _f32 and sin.dtype is _f32 and pos.dtype is _i32
+            and pos.is_contiguous() and cos.is_contiguous() and sin.is_contiguous()
+            and device == Y.get_device() == pos.get_device() == cos.get_device() == sin.get_device() == _get_device()):
+        number = _check_rope(desc, X, pos, cos, sin, Y)
+    st = lib().dg_rope(desc.handle, number, X.data_ptr(), xs[0], xs[1], Y.data_ptr(), ys[0], ys[1], pos.data_ptr(),
+                       cos.data_ptr(), sin.data_ptr(), table[0], shape[0], shape[1], 1 if inverse else 0,
+                       _stream(stream))
     if st != DG_OK:
         raise DgError(st, "dg_rope")
     return Y
@@ -788,6 +806,28 @@ class KvCache:
         self.ref = ctypes.addressof(c)
         # the type that goes in (and that attention's queries have)
         self.in_type = torch.float16 if K.dtype is torch.float16 else torch.bfloat16
+        self.in_kind = 2 if K.dtype is torch.float16 else 1
+        self.rows = torch.Size((self.heads, self.dim))
+
+
+def _check_append(K, V, slots, cache):
+    _check_heads(K, cache.dim, "K")
+    _check_heads(V, cache.dim, "V")
+    kind = cache.in_type
+    _need(K.shape == V.shape and K.shape[1] == cache.heads and K.dtype is kind and V.dtype is kind,
+          "K and V must be (tokens, %d, %d) %s" % (cache.heads, cache.dim, kind))
+    _need(slots.dtype is _i64 and slots.is_contiguous() and slots.shape == K.shape[:1],
+          "slots must be %d contiguous int64" % K.shape[0])
+    _need(cache.device == _get_device(), "the cache must be on the current GPU")
+    _here(K, V, slots)
+
+
+def _check_queries(Q, Qout, T, cache):
+    _check_heads(Q, cache.dim, "Q")
+    _check_heads(Qout, cache.dim, "Qout")
+    _need(Q.shape[0] == T and Qout.shape == Q.shape and Q.dtype is cache.in_type and Qout.dtype is cache.in_type,
+          "Q and Qout must be (%d, q_heads, %d) %s" % (T, cache.dim, cache.in_type))
+    _here(Q, Qout)
 
 
 def dg_kv_append(desc, K, V, pos, cos, sin, slots, cache: KvCache, Q=None, Qout=None, stream=None):
@@ -796,38 +836,38 @@ def dg_kv_append(desc, K, V, pos, cos, sin, slots, cache: KvCache, Q=None, Qout=
     slot slots[t] (int64, page * page size + place; one outside the cache is left
     out).  K, V (T, heads, dim) of the cache's type (bf16 over e4m3); with Q (T,
     q_heads, dim) its heads turned into Qout, which may be Q."""
-    import torch
-    _check_heads(K, cache.dim, "K")
-    _check_heads(V, cache.dim, "V")
-    T = K.shape[0]
-    kind = cache.in_type
-    _need(K.shape == V.shape and K.shape[1] == cache.heads and K.dtype is kind and V.dtype is kind,
-          "K and V must be (tokens, %d, %d) %s" % (cache.heads, cache.dim, kind))
-    _need(slots.dtype is torch.int64 and slots.is_contiguous() and tuple(slots.shape) == (T,),
-          "slots must be %d contiguous int64" % T)
-    _need((Q is None) == (Qout is None) and (Q is None or desc is not None), "Q turns into Qout by desc")
     if _tensor is None:
         _bind_torch()
-    _need(cache.device == _get_device(), "the cache must be on the current GPU")
-    _here(K, V, slots)
-    p = c = s = q = qo = None
+    kind, device, shape, ks, vs = cache.in_type, cache.device, K.shape, K.stride(), V.stride()
+    # the usual call in one expression; anything else is named in _check_append
+    if not (len(shape) == 3 and shape[1:] == cache.rows and V.shape == shape and K.dtype is kind and V.dtype is kind
+            and ks[2] == 1 and vs[2] == 1 and slots.dtype is _i64 and slots.shape == shape[:1] and slots.is_contiguous()
+            and device == K.get_device() == V.get_device() == slots.get_device() == _get_device()):
+        _check_append(K, V, slots, cache)
+    p = c = s = q = qo = d = None
     rows = heads = 0
     qs = qos = (0, 0)
     if desc is not None:
-        _need(desc.dim == cache.dim, "the rotation must be of the cache's head size")
-        rows = _check_tables(desc, pos, cos, sin, T)
-        p, c, s = pos.data_ptr(), cos.data_ptr(), sin.data_ptr()
-    if Q is not None:
-        _check_heads(Q, cache.dim, "Q")
-        _check_heads(Qout, cache.dim, "Qout")
-        _need(Q.shape[0] == T and Qout.shape == Q.shape and Q.dtype is kind and Qout.dtype is kind,
-              "Q and Qout must be (%d, q_heads, %d) %s" % (T, cache.dim, kind))
-        _here(Q, Qout)
-        q, qo, heads, qs, qos = Q.data_ptr(), Qout.data_ptr(), Q.shape[1], Q.stride(), Qout.stride()
-    ks, vs = K.stride(), V.stride()
-    st = lib().dg_kv_append(desc and desc.handle, cache.ref, 2 if kind is torch.float16 else 1, q, qs[0], qs[1], qo,
-                            qos[0], qos[1], heads, K.data_ptr(), ks[0], ks[1], V.data_ptr(), vs[0], vs[1], p, c, s,
-                            rows, slots.data_ptr(), T, _stream(stream))
+        _need(pos is not None and cos is not None and sin is not None, "a rotation takes pos, cos and sin")
+        table = cos.shape
+        if not (desc.dim == cache.dim and table == sin.shape and len(table) == 2 and table[1] == desc.half
+                and pos.shape == (desc.n_axes, shape[0]) and cos.dtype is _f32 and sin.dtype is _f32
+                and pos.dtype is _i32 and pos.is_contiguous() and cos.is_contiguous() and sin.is_contiguous()
+                and device == pos.get_device() == cos.get_device() == sin.get_device()):
+            _need(desc.dim == cache.dim, "the rotation must be of the cache's head size")
+            _check_tables(desc, pos, cos, sin, shape[0])
+        d, rows, p, c, s = desc.handle, table[0], pos.data_ptr(), cos.data_ptr(), sin.data_ptr()
+    if Q is not None or Qout is not None:
+        _need(Q is not None and Qout is not None and desc is not None, "Q turns into Qout by desc")
+        qs, qos, qshape = Q.stride(), Qout.stride(), Q.shape
+        if not (len(qshape) == 3 and Qout.shape == qshape and qshape[0] == shape[0] and qshape[2] == shape[2]
+                and qs[2] == 1 and qos[2] == 1 and Q.dtype is kind and Qout.dtype is kind
+                and device == Q.get_device() == Qout.get_device()):
+            _check_queries(Q, Qout, shape[0], cache)
+        q, qo, heads = Q.data_ptr(), Qout.data_ptr(), qshape[1]
+    st = lib().dg_kv_append(d, cache.ref, cache.in_kind, q, qs[0], qs[1], qo, qos[0], qos[1], heads, K.data_ptr(),
+                            ks[0], ks[1], V.data_ptr(), vs[0], vs[1], p, c, s, rows, slots.data_ptr(), shape[0],
+                            _stream(stream))
     if st != DG_OK:
         raise DgError(st, "dg_kv_append")
     return cache
@@ -837,7 +877,7 @@ def _check_paged(desc, Q, cache, cu_q, kv_len, page_table, O):
     import torch
     _check_heads(Q, cache.dim, "Q")
     _check_heads(O, cache.dim, "O")
-    out = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[desc.fields["out"]]
+    out = _out_dtype(desc)
     _need(Q.dtype is cache.in_type, "Q must be %s" % cache.in_type)
     _need(O.shape == Q.shape and O.dtype is out, "O must have Q's shape and the descriptor's output type")
     _need(Q.shape[1] % cache.heads == 0, "Q's heads must be a multiple of the cache's")
@@ -847,6 +887,8 @@ def _check_paged(desc, Q, cache, cu_q, kv_len, page_table, O):
           tuple(cu_q.shape) == (B + 1,) and page_table.dim() == 2 and page_table.shape[0] == B and
           cu_q.is_contiguous() and kv_len.is_contiguous() and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
           "cu_q (B + 1), kv_len (B) and page_table (B, width) must be int32 with whole rows")
+    _need(cache.device == _get_device(), "the cache must be on the current GPU")
+    _here(Q, O, cu_q, kv_len, page_table)
 
 
 def dg_attention_paged_bytes(desc: AttnDesc, cache: KvCache, rows, q_heads, batch, max_q, max_kv) -> int:
@@ -867,34 +909,30 @@ def dg_attention_paged(desc: AttnDesc, Q, cache: KvCache, cu_q, kv_len, page_tab
     are the same without."""
     if _tensor is None:
         _bind_torch()
-    key = (Q.dtype, O.dtype, cu_q.dtype, kv_len.dtype, page_table.dtype)
-    qs, os_, ts = Q.shape, O.shape, page_table.shape
-    qt, ot = Q.stride(), O.stride()
+    qs, ts, device = Q.shape, page_table.shape, cache.device
+    qt, ot, tt = Q.stride(), O.stride(), page_table.stride()
+    out = desc.types
+    if out is None:
+        out = desc.types = _out_dtype(desc)
     # the usual call in one expression; anything else is named in _check_paged
-    if not (key in _paged_types.get((cache.kind, desc.fields["out"]), ()) and len(qs) == 3 and os_ == qs
-            and qs[2] == cache.dim and qt[2] == 1 and ot[2] == 1 and qs[1] % cache.heads == 0
-            and kv_len.dim() == 1 and cu_q.dim() == 1 and len(ts) == 2 and ts[0] == kv_len.shape[0]
-            and cu_q.shape[0] == ts[0] + 1 and page_table.is_contiguous() and cu_q.is_contiguous()
-            and kv_len.is_contiguous()):
+    if not (Q.dtype is cache.in_type and O.dtype is out and cu_q.dtype is _i32 and kv_len.dtype is _i32
+            and page_table.dtype is _i32 and len(qs) == 3 and O.shape == qs and qs[2] == cache.dim and qt[2] == 1
+            and ot[2] == 1 and qs[1] % cache.heads == 0 and len(ts) == 2 and tt[1] == 1 and kv_len.shape == ts[:1]
+            and cu_q.shape == (ts[0] + 1,) and cu_q.is_contiguous() and kv_len.is_contiguous()
+            and device == Q.get_device() == O.get_device() == cu_q.get_device() == kv_len.get_device()
+            == page_table.get_device() == _get_device()):
         _check_paged(desc, Q, cache, cu_q, kv_len, page_table, O)
-        _paged_types.setdefault((cache.kind, desc.fields["out"]), set()).add(key)
-    _need(cache.device == _get_device(), "the cache must be on the current GPU")
-    _here(Q, O, cu_q, kv_len, page_table)
     ws, wb = None, 0
     if workspace is not None:
         _need(workspace.element_size() == 1 and workspace.is_contiguous(), "workspace must be contiguous bytes")
         _here(workspace)
         ws, wb = workspace.data_ptr(), workspace.numel()
-    st = lib().dg_attention_paged(desc.handle, 2 if cache.kind == 2 else 1, Q.data_ptr(), qt[0], qt[1], cache.ref,
-                                  cu_q.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), ts[1],
-                                  page_table.stride(0), O.data_ptr(), ot[0], ot[1], qs[0], qs[1], ts[0], max_q,
-                                  max_kv, qk_scale, ws, wb, _stream(stream))
+    st = lib().dg_attention_paged(desc.handle, cache.in_kind, Q.data_ptr(), qt[0], qt[1], cache.ref, cu_q.data_ptr(),
+                                  kv_len.data_ptr(), page_table.data_ptr(), ts[1], tt[0], O.data_ptr(), ot[0], ot[1],
+                                  qs[0], qs[1], ts[0], max_q, max_kv, qk_scale, ws, wb, _stream(stream))
     if st != DG_OK:
         raise DgError(st, "dg_attention_paged")
     return O
-
-
-_paged_types = {}   # the tensors' types that a (cache type, output type) was called with and _check_paged took
 
 
 def exported_symbols():

@@ -266,6 +266,31 @@ def test_bits_do_not_depend_on_the_call(dg, exp2, split, dtype, cache, p):
         same(alone.run(dg, desc), want[first:end])
 
 
+@pytest.mark.parametrize("dim,Hq,Hkv,n,m,cache", [(128, 64, 8, 820, 900, None), (128, 32, 8, 820, 900, None), (128, 64, 8, 810, 811, "float8_e4m3fn"),
+                                                  (128, 16, 2, 130, 1300, None), (64, 64, 8, 820, 900, None), (64, 8, 1, 77, 2000, None)])
+@pytest.mark.parametrize("exp2", ["inst", "lib"])
+def test_bits_of_large_tiles(dg, dim, Hq, Hkv, n, m, cache, exp2):
+    """Chunks whose tiles fill the chip, and some that nearly do, over several spans: every
+    workgroup shape, against 64 bits, and the bits of single tokens and of one workgroup per row."""
+    b = Batch(dg, [n], [m], Hq, Hkv, dim, "bfloat16", cache, seed=5)
+    desc = dict(causal=1, split_keys=128, exp2=exp2)
+    got = b.run(dg, desc)
+    check(b, got, desc)
+    same(got, captured(b, dg, desc))
+    for j in (0, 1, 100 % n, n // 2, n - 1):
+        part = Batch(dg, [1], [m - n + j + 1], Hq, Hkv, dim, "bfloat16", cache, dense=([b.dense[0][:m - n + j + 1]], b.q[j:j + 1]))
+        same(part.run(dg, desc), got[j:j + 1])
+    # the same chunk beside others: fewer and other tiles
+    other = Batch(dg, [3, n, 1], [10, m, 5], Hq, Hkv, dim, "bfloat16", cache, seed=6,
+                  dense=([b.dense[0][:10], b.dense[0], b.dense[0][:5]], torch_cat(b.q[:3], b.q, b.q[:1])))
+    same(other.run(dg, desc)[3:3 + n], got)
+
+
+def torch_cat(*parts):
+    import torch
+    return torch.cat(parts)
+
+
 def test_decoding_by_appending(dg):
     """The operators together, as a program serves a prompt: a chunk is rotated and
     appended, attention reads the cache, then tokens follow one at a time from a
@@ -346,6 +371,16 @@ def test_values_that_are_not_finite(dg):
             # every key -inf: 0 / 0
             dense[:, 0] = -math.inf
             assert Batch(dg, [n], [m], H, H, dim, dense=([dense], q)).run(dg, desc).isnan().all()
+            # in a chunk of several tiles, at a value that some rows of one tile do not see
+            long = Batch(dg, [150], [300], H, H, 128, seed=2)
+            fine = long.run(dg, desc)
+            dense = long.dense[0].clone()
+            dense[210, 1, 1, 7], dense[290, 0, 0, 0] = math.nan, math.nan
+            got = Batch(dg, [150], [300], H, H, 128, dense=([dense], long.q)).run(dg, desc)
+            same(got[:60], fine[:60])
+            same(got[:140, 0], fine[:140, 0])
+            assert got[60:, 1, 7].isnan().all() and got[140:, 0].isnan().all()
+            same(got[60:, 1, 8:], fine[60:, 1, 8:])
             # a NaN key, and an infinite value, that only the last row sees
             for i, bad in ((0, math.nan), (0, math.inf), (1, math.nan), (1, math.inf)):
                 dense = base.dense[0].clone()

@@ -125,6 +125,8 @@ def test_attention_refusals():
                 dict(max_kv=-1), dict(max_kv=(1 << 31) - 1), dict(width=-1), dict(width=1 << 28), dict(tstride=7),
                 dict(qt=-1), dict(oh=-1), dict(rows=1 << 29)):
         assert attend(d, c, **bad) == dg.DG_ERR_SHAPE, bad
+    for wide in (dict(page_stride=1 << 30), dict(token_stride=1 << 27)):
+        assert attend(d, cache(**wide)) == dg.DG_ERR_SHAPE, wide
     for bad in (dict(Q=None), dict(O=None), dict(cu=None), dict(kv=None), dict(table=None), dict(O=C), dict(ot=64),
                 dict(oh=32)):
         assert attend(d, c, **bad) == dg.DG_ERR_INVALID, bad
