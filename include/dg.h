@@ -641,8 +641,9 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
  * The answer is RN32(T / L or T * RN32(1 / L)) times v_scale, rounded to
  * out_dtype; scores are scaled by RN32(qk_scale * k_scale).  While the maximum
  * is -inf, 0 is subtracted in its place.  With DG_EXP2_INST exp2 is the part's
- * v_exp_f32, mn = max(m, RN32(max_t score_t * qk_scale)) and p_t =
- * exp2(fma(score_t, qk_scale, -mn)), and qk_scale has to be above 0.  So the
+ * v_exp_f32, a block's mn is x = RN32(max_t score_t * qk_scale) where x > RN32(m +
+ * 8) and else m (so p_t is at most about 256), p_t = exp2(fma(score_t, qk_scale,
+ * -mn)), and qk_scale has to be above 0.  So the
  * bits of a row depend on its query, the keys that it sees and the
  * descriptor, not on the batch, the chunk that it came in, the pages or the
  * launch, and with split_keys 0 and DG_EXP2_LIB are dg_attention's.

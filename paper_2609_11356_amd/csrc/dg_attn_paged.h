@@ -19,8 +19,9 @@
 // once for all the query heads of a key head.
 //
 // exp2 "inst" (INST) takes the part's own exponential and joins the scale to
-// the subtraction: p_t = v_exp(fma(score_t, qk_scale, -mn)), mn the rounded
-// product of the largest score; 7 VALU slots a score instead of 16.
+// the subtraction: p_t = v_exp(fma(score_t, qk_scale, -mn)), with mn the rounded
+// product of the block's largest score where that exceeds m by more than 8, else
+// m; 7 VALU slots a score instead of 16.
 #pragma once
 
 #include "dg_attn_tile.h"
@@ -159,6 +160,12 @@ struct Row {
   }
 };
 
+// INST: how far above the value that is subtracted a score may lie before that
+// moves.  2^8 times the largest of the types' probabilities leaves their precision
+// and range as they are, and the output is rescaled about once a span, not with
+// every block in which one of a wave's rows meets a new maximum.
+constexpr float SLACK = 8.0f;
+
 // The state of a wave's RW rows over transposed score tiles, as in attn_fwd_t
 // (dg_attn.hip): a lane owns one row (lane % RW), G = lane / RW names its share of
 // the keys, P~ stays in registers.  KT: the cache's elements, 0 bf16, 1 binary16,
@@ -184,12 +191,18 @@ struct PagedTile {
   static constexpr __device__ int tile_key(int t) { return RW == 32 ? 32 * t : 32 * (t >> 1) + 4 * (t & 1); }
   // score register i of the lane: the key (relative to 8 G)
   static constexpr __device__ int key_of(int i) { return KS * (i >> 3) + (i & 7); }
-  // the lane's place in V rows in LDS for output tile dt (elements; key steps add
-  // constants, which leave the swizzle as it is)
-  static __device__ __forceinline__ int v_place(int lane, int dt) {
+  // the lane's place in V rows in LDS for output tile 0 (elements; tile dt: ^ RW dt;
+  // key steps add constants, which leave the swizzle as it is)
+  static __device__ __forceinline__ int v_place(int lane) {
     const int vi = lane & 15, vrow = (RW == 32 ? 8 * (lane >> 5) : 8 * (lane >> 4)) + (vi >> 2);
     const int vcol = (RW == 32 ? 16 * ((lane >> 4) & 1) : 0) + 4 * (vi & 3);
-    return 8 * (vrow * DC + (((RW * dt + vcol) >> 3) ^ v_swz<RW, DC>(vrow))) + (vcol & 7);
+    return 8 * (vrow * DC + ((vcol >> 3) ^ v_swz<RW, DC>(vrow))) + (vcol & 7);
+  }
+  // the same in K rows for head-dimension step 0 (step k: ^ 8 (KS / 8) k; tiles add
+  // tile_key D)
+  static __device__ __forceinline__ int k_place(int lane) {
+    const int kmap = key_of_row<RW>(lane & (RW - 1));
+    return 8 * (kmap * DC + ((lane / RW) ^ k_swz<RW, DC>(kmap)));
   }
 
   __device__ __forceinline__ void start_span() {
@@ -229,11 +242,50 @@ struct PagedTile {
     mma<F16>(Sn[t], k, q);
   }
 
-  // One key block from key kb, its scores in Sn and its V rows at V_ (places
-  // vad); next(u) runs score instruction u of the block after it.
-  template <typename Next>
-  __device__ __forceinline__ void block(const PagedArgs& a, int kb, int vis, int vis_least, int G,
-                                        lds_u16 V_, const int* vad, Next&& next) {
+  // One key block from key kb, its scores in Sn and its V rows at V_ (the lane's
+  // place v0); load_k(u) fetches the K operand of score instruction u of the block
+  // after it, whose scores are left in Sn.
+  //
+  // The matrix instructions of a block come in one order, with the VALU's work
+  // dealt out between them: in step kk the exponentials of its KS keys, and under
+  // them the step's share of the next block's scores and P~ V of step kk - 1, in
+  // turn.  Operands are fetched AHEAD instructions before their use.  (Left to
+  // itself the compiler waits for every operand right before its instruction: 1110
+  // instead of AAAA us for a chunk of 4096 tokens over 16000 keys.)
+  static constexpr int AHEAD = KT == 2 && RW == 32 ? 1 : 2;   // (e4m3 rows on their way leave fewer registers)
+  struct Op {
+    int step;                    // the step whose exponentials it runs under (NK: after the last)
+    int place, of;               // its place among the step's instructions
+    bool v;                      // P~ V of step - 1 (index: output tile), else a score (index: u)
+    int index;
+  };
+  static constexpr int OPS = NQ + NK * ND;
+  static constexpr __device__ Op op_at(int o) {
+    constexpr int SQ = NQ / NK;
+    static_assert(SQ == ND, "scores and P~ V in turn");
+    if (o < SQ) return Op{0, o, SQ, false, o};
+    o -= SQ;
+    if (o < (NK - 1) * 2 * ND) {
+      const int step = 1 + o / (2 * ND), i = o % (2 * ND);
+      return Op{step, i, 2 * ND, i % 2 == 1, i % 2 == 1 ? i / 2 : step * SQ + i / 2};
+    }
+    o -= (NK - 1) * 2 * ND;
+    return Op{NK, o, ND, true, o};
+  }
+  template <typename LoadK>
+  __device__ __forceinline__ void block(const PagedArgs& a, int kb, int vis, int vis_least, int G, lds_u16 V_, int v0,
+                                        const shortx8* qf, LoadK&& load_k) {
+    shortx8 frag[AHEAD + 1];
+    auto fetch_op = [&](auto o) {
+      constexpr Op op = op_at(o);
+      if constexpr (op.v) {
+        const int at = (v0 ^ (RW * op.index)) + KS * (op.step - 1) * D;
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(&V_[at]));
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(&V_[at + 4 * D]));
+        frag[o % (AHEAD + 1)] = shortx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      } else frag[o % (AHEAD + 1)] = load_k(op.index);
+    };
+    static_for<0, AHEAD + 1>([&](auto o) { fetch_op(o); });
     float S[NP];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -257,7 +309,7 @@ struct PagedTile {
     halves_swap(bm, bo);
     bm = __builtin_fmaxf(bm, bo);
     if constexpr (INST) bm = bm * a.qk_scale;
-    const float mn = __builtin_fmaxf(m, bm), ms = finite_max(mn);
+    const float mn = INST ? (bm > m + SLACK ? bm : m) : __builtin_fmaxf(m, bm), ms = finite_max(mn);
     const float alpha = pow2<INST>(m - ms);
     m = mn;
     // rescale the output rows (skipped when every row of the wave keeps its
@@ -268,38 +320,35 @@ struct PagedTile {
 #pragma unroll
         for (int i = 0; i < TR; ++i) O[dt][i] = alpha * O[dt][i];
     }
-    float n8[NK];
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
+    float n8[NK], v[8];
+    shortx8 pf;
+    static_for<0, OPS>([&](auto o) {
+      constexpr Op op = op_at(o);
+      if constexpr (op.v) mma<F16>(O[op.index], frag[o % (AHEAD + 1)], pf);
+      else score(op.index, frag[o % (AHEAD + 1)], qf[op.index % QKS]);
       __builtin_amdgcn_sched_barrier(0);
-      float v[8];
+      if constexpr (o + AHEAD + 1 < OPS) fetch_op(std::integral_constant<int, o + AHEAD + 1>{});
+      if constexpr (op.step < NK) {
+        constexpr int e0 = 8 * op.place / op.of, e1 = 8 * (op.place + 1) / op.of;
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        v[e] = pow2<INST>(INST ? __builtin_fmaf(S[8 * kk + e], a.qk_scale, -ms) : S[8 * kk + e] - ms);
-      // P~ = p narrowed, already in operand layout
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = narrow2<F16>(v[2 * e], v[2 * e + 1]);
-      const shortx8 pf = __builtin_bit_cast(shortx8, w);
-      // the perfect tree over the block's keys in order
-#pragma unroll
-      for (int x = 1; x < 8; x <<= 1)
-#pragma unroll
-        for (int e = 0; e < 8; e += 2 * x) v[e] = v[e] + v[e + x];
-      n8[kk] = v[0];
-      // the next block's scores, then O^T = alpha O^T (+) V^T P~^T: for each
-      // output the steps of KS keys in increasing order
-#pragma unroll
-      for (int u = kk * NQ / NK; u < (kk + 1) * NQ / NK; ++u) next(u);
-      if constexpr (RW == 16) __builtin_amdgcn_sched_barrier(0);   // (fewer fragments at once: registers)
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) {
-        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(&V_[vad[dt] + KS * kk * D]));
-        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(&V_[vad[dt] + (KS * kk + 4) * D]));
-        mma<F16>(O[dt], shortx8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, pf);
+        for (int e = e0; e < e1; ++e)
+          v[e] = pow2<INST>(INST ? __builtin_fmaf(S[8 * op.step + e], a.qk_scale, -ms) : S[8 * op.step + e] - ms);
       }
-    }
-    __builtin_amdgcn_sched_barrier(0);
+      if constexpr (op.step < NK && op.place == op.of - 1) {
+        // P~ = p narrowed, already in operand layout
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = narrow2<F16>(v[2 * e], v[2 * e + 1]);
+        pf = __builtin_bit_cast(shortx8, w);
+        // the perfect tree over the block's keys in order
+#pragma unroll
+        for (int x = 1; x < 8; x <<= 1)
+#pragma unroll
+          for (int e = 0; e < 8; e += 2 * x) v[e] = v[e] + v[e + x];
+        n8[op.step] = v[0];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
     if constexpr (RW == 32) {
       // one swap turns two values spread over the halves into their two sums:
       // 2^j values -> 2^(j-1) registers (one per half), down to the root

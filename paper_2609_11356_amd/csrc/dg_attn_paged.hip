@@ -13,7 +13,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 4
 attn_paged(PagedArgs a) {
   typedef PagedTile<D, KT, RW, INST, JOINS, TL> Tile;
   constexpr bool F16 = KT == 1, E8 = KT == 2;
-  constexpr int W = Tile::W, DC = Tile::DC, QKS = Tile::QKS, ND = Tile::ND, NQ = Tile::NQ;
+  constexpr int W = Tile::W, DC = Tile::DC, QKS = Tile::QKS, NQ = Tile::NQ;
   constexpr int MC = E8 ? D / 16 : DC;                     // 16-byte pieces of a row in the cache
   constexpr int NLD = W * MC / (64 * NW);                  // K (and V) loads per wave and block, 1 KB each
   static_assert(NLD >= 1 && W * MC % (64 * NW) == 0, "whole loads per wave");
@@ -57,15 +57,7 @@ attn_paged(PagedArgs a) {
   const int vis = valid ? visible(a, sq, tok) : end;
   const int vis_least = __builtin_amdgcn_readfirstlane(vis);   // no row of the wave sees fewer (or none is valid)
 
-  // the lane's fragment addresses (elements; tiles and key steps add constants,
-  // which leave the swizzles as they are)
-  const int kmap = key_of_row<RW>(li);
-  constexpr int CPS = Tile::KS / 8;              // chunks per head-dimension step
-  int kad[QKS], vad[ND];
-#pragma unroll
-  for (int k = 0; k < QKS; ++k) kad[k] = 8 * (kmap * DC + ((CPS * k + G) ^ k_swz<RW, DC>(kmap)));
-#pragma unroll
-  for (int dt = 0; dt < ND; ++dt) vad[dt] = Tile::v_place(lane, dt);
+  const int k0 = Tile::k_place(lane), v0 = Tile::v_place(lane);
 
   shortx8 qf[QKS];
   const uint16_t* Qr = a.Q + (int64_t)(sq.q0 + tok) * a.q_token + head * a.q_head;
@@ -123,8 +115,8 @@ attn_paged(PagedArgs a) {
       }
     }
   };
-  auto score = [&](lds_u16 K_, int u) {
-    t.score(u, *(const lds_s8*)&K_[kad[u % QKS] + Tile::tile_key(u / QKS) * D], qf[u % QKS]);
+  auto load_k = [&](lds_u16 K_, int base, int u) {
+    return *(const lds_s8*)&K_[(base ^ (Tile::KS * (u % QKS))) + Tile::tile_key(u / QKS) * D];
   };
 
   // P~ is 0 where a row does not see a key, and so is 0 x V, but for an infinity
@@ -170,7 +162,9 @@ attn_paged(PagedArgs a) {
       fetch(true, Vn, b + 1);
       ask();
     }
-    t.block(a, W * b, vis, vis_least, G, Vc, vad, [&](int u) { score(Kn, u); });
+    int k1 = k0, v1 = v0;
+    asm volatile("" : "+v"(k1), "+v"(v1));       // (their steps worked out per block: registers)
+    t.block(a, W * b, vis, vis_least, G, Vc, v1, qf, [&](int u) { return load_k(Kn, k1, u); });
     if constexpr (JOINS) if (b + 1 - folded == a.span_blocks || b + 1 == b1) {
       t.fold(W * folded, vis);
       folded = b + 1;
@@ -203,7 +197,7 @@ attn_paged(PagedArgs a) {
       ask();
     }
 #pragma unroll
-    for (int u = 0; u < NQ; ++u) score((lds_u16)K0, u);
+    for (int u = 0; u < NQ; ++u) t.score(u, load_k((lds_u16)K0, k0, u), qf[u % QKS]);
     for (int b = b0; whole && b < b1; b += 2) {
       whole = step(b, (lds_u16)V0, (lds_u16)V1, (lds_u16)K0, (lds_u16)K1);
       if (whole && b + 1 < b1) whole = step(b + 1, (lds_u16)V1, (lds_u16)V0, (lds_u16)K1, (lds_u16)K0);
@@ -330,8 +324,13 @@ hipError_t launch_tile(const PagedArgs& a, int nw, int rw, hipStream_t st) {
   }
   if (!joins) return launch_one<D, KT, 4, 32, INST, false, 0>(a, st);
   if constexpr (D == 64) return launch_one<D, KT, 4, 32, INST, true, 0>(a, st);
-  else if (nw == 8) return launch_one<D, KT, 8, 32, INST, true, 44>(a, st);
-  else return launch_one<D, KT, 4, 32, INST, true, 64>(a, st);
+  else {
+    // (nor for e4m3 rows on their way besides)
+    if constexpr (KT != 2) {
+      if (nw == 8) return launch_one<D, KT, 8, 32, INST, true, 44>(a, st);
+    }
+    return launch_one<D, KT, 4, 32, INST, true, 64>(a, st);
+  }
 }
 
 template <int D, bool INST>

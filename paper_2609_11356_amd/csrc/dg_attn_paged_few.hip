@@ -17,7 +17,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KT == 2 && D
 attn_paged_few(PagedArgs a) {
   typedef PagedTile<D, KT, 16, INST, false> Tile;
   constexpr bool F16 = KT == 1, E8 = KT == 2;
-  constexpr int W = Tile::W, DC = Tile::DC, QKS = Tile::QKS, ND = Tile::ND, NQ = Tile::NQ, NT = Tile::NT;
+  constexpr int W = Tile::W, DC = Tile::DC, QKS = Tile::QKS, NQ = Tile::NQ, NT = Tile::NT;
   constexpr int MC = E8 ? D / 16 : DC;                     // 16-byte pieces of a row in the cache
   constexpr int NLD = W * MC / 64;                         // loads of a V block, 1 KB each
   typedef std::conditional_t<E8, u32x2, shortx8> k_t;      // 8 elements of a K row
@@ -76,9 +76,7 @@ attn_paged_few(PagedArgs a) {
       qf[k] = *(const shortx8*)&Qr[32 * k + 8 * G];   // (rows that are not there: the first one's)
 
     const int kmap = key_of_row<16>(li);
-    int vad[ND];
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt) vad[dt] = Tile::v_place(lane, dt);
+    const int v0 = Tile::v_place(lane);
 
     Tile tile;
     tile.start();
@@ -119,12 +117,12 @@ attn_paged_few(PagedArgs a) {
         }
       }
     };
-    auto score = [&](const k_t* kk, int u) {
+    auto load_k = [&](const k_t* kk, int u) {
       if constexpr (E8) {
         const u32x4 w = {e4m3x2_bf16x2<false>(kk[u][0]), e4m3x2_bf16x2<true>(kk[u][0]), e4m3x2_bf16x2<false>(kk[u][1]),
                          e4m3x2_bf16x2<true>(kk[u][1])};
-        tile.score(u, __builtin_bit_cast(shortx8, w), qf[u % QKS]);
-      } else tile.score(u, kk[u], qf[u % QKS]);
+        return __builtin_bit_cast(shortx8, w);
+      } else return kk[u];
     };
     // block b: its K rows were in kc, the next block's are in kn
     auto step = [&](int b, lds_u16 Vc, lds_u16 Vn, k_t* kc, const k_t* kn) {
@@ -142,7 +140,7 @@ attn_paged_few(PagedArgs a) {
         for (int i = lane; i < W * DC; i += 64) bad |= not_finite<F16>(*(const lds_x4*)&Vc[8 * i]);
         if (__builtin_amdgcn_ballot_w64(bad != 0)) return false;
       }
-      tile.block(a, W * b, vis, vis_first, G, Vc, vad, [&](int u) { score(kn, u); });
+      tile.block(a, W * b, vis, vis_first, G, Vc, v0, qf, [&](int u) { return load_k(kn, u); });
       return true;
     };
     bool whole = true;
@@ -153,7 +151,7 @@ attn_paged_few(PagedArgs a) {
       locate(b0 + 1, row1);
       fetch_k(kB, b0 + 1);
 #pragma unroll
-      for (int u = 0; u < NQ; ++u) score(kA, u);
+      for (int u = 0; u < NQ; ++u) tile.score(u, load_k(kA, u), qf[u % QKS]);
       for (int b = b0; whole && b < b1; b += 2) {
         whole = step(b, (lds_u16)V0, E8 ? (lds_u16)V0 : (lds_u16)V1, kA, kB);
         if (whole && b + 1 < b1) whole = step(b + 1, E8 ? (lds_u16)V0 : (lds_u16)V1, (lds_u16)V0, kB, kA);
