@@ -601,7 +601,7 @@ typedef struct {
   int32_t dtype;             /* DG_BF16, DG_F16 or DG_E4M3 */
   void* K;                   /* device, 16-byte aligned, like V */
   void* V;
-  int64_t pages, page, heads, dim;
+  int64_t pages, page, heads, dim;                  /* pages * page below 2^31 */
   int64_t page_stride, token_stride, head_stride;   /* whole 16-byte pieces */
   float k_scale, v_scale;    /* finite and above 0 */
 } dg_kv_cache;

@@ -1363,11 +1363,27 @@ bool wide_rotation(const dg::RopeArgs& a, int pv) {
   return a.half % pv == 0 && (a.dim - 2 * a.half) % pv == 0 && (!a.half || (aligned(a.cos_t, 16) && aligned(a.sin_t, 16)));
 }
 
+// n / d for n < 2^31 as (2 n * mul >> 32) >> shift: with 2^(s - 1) < d <= 2^s and mul =
+// floor(2^(31 + s) / d) + 1 the product is off by less than 2^(31 + s) / d, as mul * d
+// exceeds 2^(31 + s) by at most d <= 2^s
+void divide_by(int64_t d, uint32_t* mul, uint32_t* shift) {
+  uint32_t s = 0;
+  while (((int64_t)1 << s) < d) ++s;
+  *mul = (uint32_t)((((uint64_t)1 << (31 + s)) / (uint64_t)d) + 1);
+  *shift = s;
+}
+
+// 1 / scale where x * (1 / scale) is x / scale to the bit (both scale by a power of two), else 0.
+float exact_inverse(float scale) {
+  int e;
+  return std::frexp(scale, &e) == 0.5f && e > -100 && e < 100 ? 1.0f / scale : 0.f;
+}
+
 dg_status check_cache(const dg_kv_cache* c) {
   if (!c || c->struct_size < sizeof(dg_kv_cache)) return DG_ERR_INVALID;
   if (c->dtype != DG_BF16 && c->dtype != DG_F16 && c->dtype != DG_E4M3) return DG_ERR_INVALID;
   if (c->pages < 1 || c->page < 1 || c->heads < 1 || c->dim < 1 || c->pages > INT32_MAX || c->page > INT32_MAX ||
-      c->heads > 65535 || c->dim > DG_ROPE_MAX_DIM)
+      c->heads > 65535 || c->dim > DG_ROPE_MAX_DIM || c->pages * c->page > INT32_MAX)
     return DG_ERR_SHAPE;
   if (!stride_ok(c->page_stride) || !stride_ok(c->token_stride) || !stride_ok(c->head_stride)) return DG_ERR_SHAPE;
   if (!c->K || !c->V) return DG_ERR_INVALID;
@@ -1440,8 +1456,11 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
   a.head_stride = c->head_stride;
   a.n_slots = c->pages * c->page;
   a.page_size = (int32_t)c->page;
+  divide_by(c->page, &a.page_mul, &a.page_shift);
   a.k_scale = c->k_scale;
   a.v_scale = c->v_scale;
+  a.k_inv = exact_inverse(c->k_scale);
+  a.v_inv = exact_inverse(c->v_scale);
   // the cache's rows are whole pieces already (check_cache)
   const bool wide = (!q_heads || (q.pieces() && qo.pieces())) && k.pieces() && v.pieces() && wide_rotation(a, 8);
   return dg::launch_rope(a, wide, (hipStream_t)stream) == hipSuccess ? DG_OK : DG_ERR_HIP;
@@ -1581,11 +1600,7 @@ dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void*
   a.pages = (int32_t)c->pages;
   a.page_size = (int32_t)c->page;
   a.kv_cap = (int32_t)std::min(max_kv, table_width * c->page);
-  // key / page for key < 2^31: with 2^(s - 1) < page <= 2^s and mul = floor(2^(31 + s)
-  // / page) + 1 the product is off by less than 2^(31 + s) / page, as mul * page
-  // exceeds 2^(31 + s) by at most page <= 2^s
-  while (((int64_t)1 << a.page_shift) < c->page) ++a.page_shift;
-  a.page_mul = (uint32_t)((((uint64_t)1 << (31 + a.page_shift)) / (uint64_t)c->page) + 1);
+  divide_by(c->page, &a.page_mul, &a.page_shift);
   a.page_step = (int32_t)(64 / c->page);
   a.page_rest = (int32_t)(64 % c->page);
   a.max_q = (int32_t)max_q;

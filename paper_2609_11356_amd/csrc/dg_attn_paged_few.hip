@@ -13,7 +13,7 @@
 namespace dg {
 
 template <int D, int KT, bool INST>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KT == 2 && D == 64 ? 2 : 1))) void
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(KT == 2 && (INST || D == 64) ? 2 : 1))) void
 attn_paged_few(PagedArgs a) {
   typedef PagedTile<D, KT, 16, INST, false> Tile;
   constexpr bool F16 = KT == 1, E8 = KT == 2;
@@ -140,7 +140,9 @@ attn_paged_few(PagedArgs a) {
         for (int i = lane; i < W * DC; i += 64) bad |= not_finite<F16>(*(const lds_x4*)&Vc[8 * i]);
         if (__builtin_amdgcn_ballot_w64(bad != 0)) return false;
       }
-      tile.block(a, W * b, vis, vis_first, G, Vc, v0, qf, [&](int u) { return load_k(kn, u); });
+      int v1 = v0;
+      asm volatile("" : "+v"(v1));               // (its steps worked out per block: registers)
+      tile.block(a, W * b, vis, vis_first, G, Vc, v1, qf, [&](int u) { return load_k(kn, u); });
       return true;
     };
     bool whole = true;

@@ -143,7 +143,8 @@ struct RopeArgs {
   int32_t in_dtype, kv_dtype, append;
   int64_t page_stride, token_stride, head_stride, n_slots;   // the cache, in elements
   int32_t page_size;
-  float k_scale, v_scale;
+  uint32_t page_mul, page_shift;   // slot / page_size, as PagedArgs
+  float k_scale, v_scale, k_inv, v_inv;   // 1 / scale where a product with it has the quotient's bits, else 0
   uint32_t axis[16];             // two bits per pair
 };
 hipError_t launch_rope(const RopeArgs& a, bool wide, hipStream_t s);

@@ -42,21 +42,33 @@ __device__ __forceinline__ void put(uint16_t* p, const float* y, int32_t dtype) 
   *(Pack<uint16_t, N>*)p = o;
 }
 
-// y / scale rounded once to e4m3, cut to +-448 (a NaN stays one).
-__device__ __forceinline__ uint8_t f32_e4m3(float y, float scale) {
-  float x = y / scale;
-  x = x > 448.0f ? 448.0f : x < -448.0f ? -448.0f : x;
-  return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
+// y / scale cut to +-448 (a NaN stays one).  inv: 1 / scale where that is exact and
+// gives the quotient's bits (a power of two), else 0.
+__device__ __forceinline__ float scaled(float y, float scale, float inv) {
+  const float x = inv != 0.f ? y * inv : y / scale;
+  return x > 448.0f ? 448.0f : x < -448.0f ? -448.0f : x;
 }
 
-// N elements of a row of the cache at element offset `at`.
+// N elements of a row of the cache at element offset `at`, e4m3 rounded once.
 template <int N>
-__device__ __forceinline__ void put_cache(void* base, int64_t at, const float* y, int32_t dtype, float scale) {
+__device__ __forceinline__ void put_cache(void* base, int64_t at, const float* y, int32_t dtype, float scale,
+                                          float inv) {
   if (dtype == DG_E4M3) {
-    Pack<uint8_t, N> o;
+    if constexpr (N == 8) {
+      uint32_t w[2];
 #pragma unroll
-    for (int e = 0; e < N; ++e) o.v[e] = f32_e4m3(y[e], scale);
-    *(Pack<uint8_t, N>*)((uint8_t*)base + at) = o;
+      for (int h = 0; h < 2; ++h) {
+        int x = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(y[4 * h], scale, inv), scaled(y[4 * h + 1], scale, inv), 0, false);
+        w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(y[4 * h + 2], scale, inv), scaled(y[4 * h + 3], scale, inv), x, true);
+      }
+      *(uint2*)((uint8_t*)base + at) = uint2{w[0], w[1]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float x = scaled(y[e], scale, inv);
+        ((uint8_t*)base)[at + e] = (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
+      }
+    }
   } else put<N>((uint16_t*)base + at, y, dtype);
 }
 
@@ -75,24 +87,35 @@ __global__ __launch_bounds__(256) void rope(RopeArgs a, int tokens, int gq, int 
     if (t >= a.T) break;
     const int gr = w % per / units, u = w % units;
     const bool is_q = gr < gq, is_v = gr >= gq + gk;
-    const RopeHeads& h = is_q ? a.q : is_v ? a.v : a.k;
+    // (selects: the three places are uniform, the choice is not)
     const int head0 = (is_q ? gr : is_v ? gr - gq - gk : gr - gq) * HPT;
+    const int heads = is_q ? a.q.heads : a.k.heads;
+    const int64_t x_head = is_q ? a.q.x_head : is_v ? a.v.x_head : a.k.x_head;
+    const E* X = (const E*)(is_q ? a.q.X : is_v ? a.v.X : a.k.X) +
+                 t * (is_q ? a.q.x_token : is_v ? a.v.x_token : a.k.x_token);
     int64_t at = 0;
     if (!is_q) {
       const int64_t slot = a.slots[t];
       if (slot < 0 || slot >= a.n_slots) continue;
-      const int64_t page = slot / a.page_size;
-      at = page * a.page_stride + (slot - page * a.page_size) * a.token_stride;
+      const uint32_t page = __umulhi(2u * (uint32_t)slot, a.page_mul) >> a.page_shift;
+      at = (int64_t)page * a.page_stride + (int64_t)((uint32_t)slot - page * (uint32_t)a.page_size) * a.token_stride;
     }
-    const E* X = (const E*)h.X + t * h.x_token;
-    E* Y = (E*)h.Y + t * h.y_token;
-    const float scale = is_v ? a.v_scale : a.k_scale;
+    E* Y = (E*)a.q.Y + t * a.q.y_token;
+    void* cache = is_v ? a.v.Y : a.k.Y;
+    const float scale = is_v ? a.v_scale : a.k_scale, inv = is_v ? a.v_inv : a.k_inv;
     // where the unit's two runs of PV elements lie (adjacent pairs, and what is
     // not turned: one run of 2 PV)
     const bool turn = u < u_rot && !is_v;
     const int e0 = u < u_rot ? (a.adjacent || is_v ? 2 * PV * u : PV * u) : 2 * a.half + 2 * PV * (u - u_rot);
     const int e1 = u < u_rot && !a.adjacent && !is_v ? e0 + a.half : e0 + PV;
     const bool second = e1 < a.dim;                          // a last short unit has one run only
+    Pack<E, PV> x0[HPT], x1[HPT];
+#pragma unroll
+    for (int n = 0; n < HPT; ++n)
+      if (head0 + n < heads) {
+        x0[n] = *(const Pack<E, PV>*)&X[(head0 + n) * x_head + e0];
+        if (second) x1[n] = *(const Pack<E, PV>*)&X[(head0 + n) * x_head + e1];
+      }
     float c[PV], s[PV];
     if (turn) {
       const int i0 = PV * u;
@@ -131,16 +154,9 @@ __global__ __launch_bounds__(256) void rope(RopeArgs a, int tokens, int gq, int 
 #pragma unroll
         for (int e = 0; e < PV; ++e) s[e] = -s[e];
     }
-    Pack<E, PV> x0[HPT], x1[HPT];
-#pragma unroll
-    for (int n = 0; n < HPT; ++n)
-      if (head0 + n < h.heads) {
-        x0[n] = *(const Pack<E, PV>*)&X[(head0 + n) * h.x_head + e0];
-        if (second) x1[n] = *(const Pack<E, PV>*)&X[(head0 + n) * h.x_head + e1];
-      }
 #pragma unroll
     for (int n = 0; n < HPT; ++n) {
-      if (head0 + n >= h.heads) break;
+      if (head0 + n >= heads) break;
       float y0[PV], y1[PV];
 #pragma unroll
       for (int e = 0; e < PV; ++e) {
@@ -174,13 +190,13 @@ __global__ __launch_bounds__(256) void rope(RopeArgs a, int tokens, int gq, int 
         }
       }
       if (is_q) {
-        E* y = Y + (head0 + n) * h.y_head;
+        E* y = Y + (head0 + n) * a.q.y_head;
         put<PV>(y + e0, y0, a.in_dtype);
         if (second) put<PV>(y + e1, y1, a.in_dtype);
       } else {
         const int64_t row = at + (head0 + n) * a.head_stride;
-        put_cache<PV>(h.Y, row + e0, y0, a.kv_dtype, scale);
-        if (second) put_cache<PV>(h.Y, row + e1, y1, a.kv_dtype, scale);
+        put_cache<PV>(cache, row + e0, y0, a.kv_dtype, scale, inv);
+        if (second) put_cache<PV>(cache, row + e1, y1, a.kv_dtype, scale, inv);
       }
     }
   }

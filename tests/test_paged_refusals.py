@@ -70,7 +70,7 @@ def cache(**f):
 BAD_CACHES = [(dict(struct_size=8), 1), (dict(dtype=0), 1), (dict(dtype=4), 1), (dict(K=None), 1), (dict(V=None), 1),
               (dict(k_scale=0.5), 1), (dict(dtype=3, k_scale=0.0), 1), (dict(dtype=3, v_scale=float("nan")), 1),
               (dict(dtype=3, v_scale=float("inf")), 1), (dict(dtype=3, k_scale=-1.0), 1),
-              (dict(pages=0), 3), (dict(page=0), 3), (dict(heads=0), 3), (dict(dim=0), 3), (dict(page_stride=-16), 3),
+              (dict(pages=0), 3), (dict(pages=1 << 27), 3), (dict(page=0), 3), (dict(heads=0), 3), (dict(dim=0), 3), (dict(page_stride=-16), 3),
               (dict(K=A + 8), 4), (dict(V=B + 2), 4), (dict(token_stride=132), 4), (dict(head_stride=68), 4),
               (dict(page_stride=2052), 4), (dict(dtype=3, head_stride=72), 4)]
 
