@@ -1493,7 +1493,7 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
   std::memset(&p, 0, sizeof p);
   const int64_t g = q_heads / c->heads, most = max_q * g, split = d->p.split_keys;
   p.nspan = split ? (int32_t)((max_kv + split - 1) / split) : 1;
-  const bool spans = p.nspan > 1 && p.nspan <= 65535;
+  const bool spans = p.nspan > 1 && p.nspan <= 65535 && (int64_t)p.nspan * batch * c->heads < PAGED_SIZES;
   if (most <= 16 || batch > 1) {
     PagedLaunch& l = p.l[p.n++];
     l = PagedLaunch{1, 16, 0, 16, (int32_t)std::min<int64_t>(most, 16), spans, 0};

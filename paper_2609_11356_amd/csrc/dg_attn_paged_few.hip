@@ -25,7 +25,14 @@ attn_paged_few(PagedArgs a) {
   __shared__ __attribute__((aligned(1024))) uint16_t V1[E8 ? 8 : W * D];
   __shared__ RowAddress where[4][W];
 
-  const int kvh = blockIdx.x % a.Hkv, span = blockIdx.y, bat = blockIdx.z;
+  // `near` key heads of a span go to one XCD (workgroup i runs on XCD i % 8), one after
+  // the other.  The spans' order turns from sequence to sequence, so that short ones
+  // load all XCDs.
+  const uint32_t near = a.near, sets = (uint32_t)a.Hkv / near, turn = blockIdx.x / 8;
+  const uint32_t set = blockIdx.x % 8 + 8 * (turn / near), group = set / sets, spans = a.rec ? a.nspan : 1;
+  const int kvh = (int)(near * (set % sets) + turn % near), bat = (int)(group / spans);
+  const int span = (int)((near > 1 ? group + 3u * bat : group) % spans);
+  if (bat >= a.B) return;
   const Seq sq = sequence(a, bat);
   const int nrow = rows_of(a, sq);
   if (nrow <= a.row_lo || nrow > a.row_hi || nrow > 16) return;
@@ -181,9 +188,28 @@ attn_paged_few(PagedArgs a) {
 
 namespace {
 
+// Key heads of one span that go to one XCD.  A token's heads lie side by side in most
+// caches, and memory is read the faster the nearer in time its neighbours are: where
+// there is work for some rounds of the chip, up to 1 KB of heads of at most 128
+// bytes (128 sequences of 1000 to 16000 keys, 8 heads of 128 e4m3 bytes: 1 head 522
+// us, 2 497, 4 478, 8 437), or 512 bytes of larger ones (64 of 200 to 8000, 256 bytes: 1
+// head 218 us, 2 or more 209; 4 of 60000 to 131072: 281, 282 and, by 4, 287).  Less
+// work takes the XCDs in turn, which loads them more evenly (32 sequences of 300 to
+// 4500 keys: 17 us, near by 20).
+int near_heads(const PagedArgs& a, int64_t spans) {
+  const int64_t piece = a.dim * (a.kv_dtype == DG_E4M3 ? 1 : 2), most = piece <= 128 ? 1024 : 512;
+  int n = 1;
+  if (spans * a.B * a.Hkv >= 4096)
+    while (a.Hkv % (2 * n) == 0 && 2 * n * piece <= most) n *= 2;
+  return n;
+}
+
 template <int D, int KT, bool INST>
-hipError_t launch_few(const PagedArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)a.Hkv, (unsigned)(a.rec ? a.nspan : 1), (unsigned)a.B);
+hipError_t launch_few(PagedArgs a, hipStream_t st) {
+  const int64_t spans = a.rec ? a.nspan : 1;
+  a.near = near_heads(a, spans);
+  const int64_t sets = spans * a.B * (a.Hkv / a.near);
+  const dim3 grid((unsigned)((sets + 7) / 8 * 8 * a.near));
   hipLaunchKernelGGL((attn_paged_few<D, KT, INST>), grid, dim3(64), 0, st, a);
   return hipGetLastError();
 }

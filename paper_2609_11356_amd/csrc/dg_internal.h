@@ -115,6 +115,7 @@ struct PagedArgs {
   int32_t page_step, page_rest;       // 64 / page_size and 64 % page_size
   int32_t max_q, span_blocks, nspan;  // blocks of 64 keys per span; spans of max_kv keys
   int32_t row_lo, row_hi;        // sequences with row_lo < new tokens * g <= row_hi are taken
+  int32_t near;                  // few rows: key heads of a span on one XCD
   int32_t rec_rows;              // records of row r of (sequence, key head): rows reserved for each; 0: by token and head
   int32_t causal, l_fma, final_recip, out_dtype, kv_dtype, inst;
   float qk_scale, v_scale;

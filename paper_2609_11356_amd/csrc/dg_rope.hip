@@ -220,7 +220,7 @@ hipError_t launch_heads(const RopeArgs& a, hipStream_t st) {
 // wide: every row, run and stride a whole number of 16-byte pieces
 hipError_t launch_rope(const RopeArgs& a, bool wide, hipStream_t st) {
   if (a.in_dtype == DG_F32) return wide ? launch_heads<float, 4, 4>(a, st) : launch_heads<float, 1, 1>(a, st);
-  return wide ? launch_heads<uint16_t, 8, 4>(a, st) : launch_heads<uint16_t, 1, 1>(a, st);
+  return wide ? launch_heads<uint16_t, 8, 2>(a, st) : launch_heads<uint16_t, 1, 1>(a, st);
 }
 
 }  // namespace dg
