@@ -666,9 +666,9 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
  * DG_ERR_UNSUPPORTED unless key_block is 64, block_sum DG_TREE, pv_fma 1,
  * q_block (causal) a multiple of 64, dim 64 or 128, (q_dtype, cache, p_dtype)
  * are (bf16, bf16, bf16), (f16, f16, f16) or (bf16, e4m3, bf16);  DG_ERR_SHAPE
- * for sizes out of range (rows * q_heads, max_kv and table_width * page below
- * 2^31 - 1024, batch at most 65535, q_heads a multiple of the cache's heads,
- * page_stride and (page - 1) * token_stride below 2^31 bytes),
+ * for sizes out of range (rows * q_heads at most 2^28, batch 65535, batch * heads
+ * 2^24, max_kv and table_width * page below 2^31 - 1024, q_heads a multiple of
+ * the cache's heads, page_stride and (page - 1) * token_stride below 2^31 bytes),
  * DG_ERR_ALIGN, DG_ERR_INVALID as elsewhere;  DG_ERR_SCRATCH for a
  * workspace that is too small. */
 dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void* Q, int64_t q_token, int64_t q_head,

@@ -1468,7 +1468,9 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
 
 namespace {
 
-constexpr int64_t PAGED_SIZES = INT32_MAX - 1024;         // rows * heads and keys: 31-bit counts with room
+constexpr int64_t PAGED_SIZES = INT32_MAX - 1024;         // keys: 31-bit counts with room
+constexpr int64_t PAGED_ROWS = (int64_t)1 << 28;          // rows * heads: threads of a grid in 32 bits
+constexpr int64_t PAGED_WORKGROUPS = (int64_t)1 << 24;    // batch * key heads (and spans), for the same
 constexpr size_t PAGED_WORKSPACE = (size_t)1 << 30;       // more records than this: one walk per row
 
 // How a paged call is run (speed only): up to two launches, for sequences of
@@ -1492,8 +1494,8 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
   PagedPlan p;
   std::memset(&p, 0, sizeof p);
   const int64_t g = q_heads / c->heads, most = max_q * g, split = d->p.split_keys;
-  p.nspan = split ? (int32_t)((max_kv + split - 1) / split) : 1;
-  const bool spans = p.nspan > 1 && p.nspan <= 65535 && (int64_t)p.nspan * batch * c->heads < PAGED_SIZES;
+  p.nspan = split ? (int32_t)std::max<int64_t>(1, (max_kv + split - 1) / split) : 1;
+  const bool spans = p.nspan > 1 && p.nspan <= 65535 && p.nspan * batch * c->heads <= PAGED_WORKGROUPS;
   if (most <= 16 || batch > 1) {
     PagedLaunch& l = p.l[p.n++];
     l = PagedLaunch{1, 16, 0, 16, (int32_t)std::min<int64_t>(most, 16), spans, 0};
@@ -1512,6 +1514,7 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
       l.rw = 32;
       if (c->dim == 64) l.split = spans && groups(128) < 400;
       else if (groups(256) >= 200) l.nw = 8;
+      else if (groups(64) >= 400) l.rw = 16;   // (two workgroups a CU: 1023 tokens, 32 over 8 heads, 129 us, of 32 rows 151)
       else l.split = spans && groups(128) < 200;
     }
     l.records = (size_t)rows * q_heads;
@@ -1534,8 +1537,8 @@ dg_status check_paged(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows,
   if (p.key_block != 64 || p.block_sum != DG_TREE || !p.pv_fma || (p.causal && p.q_block % 64)) return DG_ERR_UNSUPPORTED;
   if (c->dim != 64 && c->dim != 128) return DG_ERR_UNSUPPORTED;
   if (p.p_dtype != (c->dtype == DG_F16 ? DG_F16 : DG_BF16)) return DG_ERR_UNSUPPORTED;
-  if (rows > PAGED_SIZES || q_heads > 65535 || rows * q_heads > PAGED_SIZES || batch > 65535 || max_kv > PAGED_SIZES ||
-      q_heads % c->heads)
+  if (rows > PAGED_ROWS || q_heads > 65535 || rows * q_heads > PAGED_ROWS || batch > 65535 ||
+      batch * c->heads > PAGED_WORKGROUPS || max_kv > PAGED_SIZES || q_heads % c->heads)
     return DG_ERR_SHAPE;
   return DG_OK;
 }

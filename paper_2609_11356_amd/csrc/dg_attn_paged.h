@@ -251,7 +251,8 @@ struct PagedTile {
   // them the step's share of the next block's scores and P~ V of step kk - 1, in
   // turn.  Operands are fetched AHEAD instructions before their use.  (Left to
   // itself the compiler waits for every operand right before its instruction: 1110
-  // instead of AAAA us for a chunk of 4096 tokens over 16000 keys.)
+  // instead of 1037 us for a chunk of 4096 tokens over 16000 keys, of 1023 over 8192
+  // in tiles of 128 rows 189 instead of 151.)
   static constexpr int AHEAD = KT == 2 && RW == 32 ? 1 : 2;   // (e4m3 rows on their way leave fewer registers)
   struct Op {
     int step;                    // the step whose exponentials it runs under (NK: after the last)

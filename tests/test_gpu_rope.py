@@ -249,6 +249,21 @@ def test_offsets_past_32_bits(dg):
     assert int((K[0] != 0).sum()) == 0 and int((K[pages // 2] != 0).sum()) == 0
 
 
+def test_more_tokens_than_workgroups(dg):
+    """2^20 workgroups take the tokens in turns."""
+    import torch
+    T, H, dim = (1 << 20) + 77, 3, 130
+    cos, sin = tables(50, 65)
+    x = torch.randn(T, H, dim, device="cuda").bfloat16()
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") % 50
+    y = dg.dg_rope(dg.RopeDesc(dim), x, pos[None], cuda(cos), cuda(sin), torch.empty_like(x))
+    for t in (0, 1, (1 << 20) - 1, 1 << 20, T - 1):
+        want = turn(host(x[t:t + 1]), np.array([[t % 50]]), cos, sin, dim, "half", None)
+        same(host(y[t:t + 1]), rounded(want, x.dtype))
+    assert bool((y[1 << 20:] == dg.dg_rope(dg.RopeDesc(dim), x[1 << 20:], pos[None, 1 << 20:].contiguous(), cuda(cos), cuda(sin),
+                                           torch.empty_like(x[1 << 20:]))).all())
+
+
 def test_refusals(dg):
     import torch
     desc = dg.RopeDesc(64)

@@ -123,8 +123,9 @@ def test_attention_refusals():
     assert attend(d, cache(dtype=2)) == dg.DG_ERR_UNSUPPORTED        # bf16 probabilities over binary16
     for bad in (dict(rows=-1), dict(heads=7), dict(heads=-2), dict(batch=-1), dict(batch=65536), dict(max_q=-1),
                 dict(max_kv=-1), dict(max_kv=(1 << 31) - 1), dict(width=-1), dict(width=1 << 28), dict(tstride=7),
-                dict(qt=-1), dict(oh=-1), dict(rows=1 << 29)):
+                dict(qt=-1), dict(oh=-1), dict(rows=1 << 29), dict(rows=(1 << 25) + 1)):
         assert attend(d, c, **bad) == dg.DG_ERR_SHAPE, bad
+    assert attend(d, cache(heads=300), heads=300, batch=60000) == dg.DG_ERR_SHAPE
     for wide in (dict(page_stride=1 << 30), dict(token_stride=1 << 27)):
         assert attend(d, cache(**wide)) == dg.DG_ERR_SHAPE, wide
     for bad in (dict(Q=None), dict(O=None), dict(cu=None), dict(kv=None), dict(table=None), dict(O=C), dict(ot=64),
