@@ -770,9 +770,9 @@ def dg_rope(desc: RopeDesc, X, pos, cos, sin, Y, inverse=False, stream=None):
             and pos.is_contiguous() and cos.is_contiguous() and sin.is_contiguous()
             and device == Y.get_device() == pos.get_device() == cos.get_device() == sin.get_device() == _get_device()):
         number = _check_rope(desc, X, pos, cos, sin, Y)
-    st = lib().dg_rope(desc.handle, number, X.data_ptr(), xs[0], xs[1], Y.data_ptr(), ys[0], ys[1], pos.data_ptr(),
+    st = (_lib or lib()).dg_rope(desc.handle, number, X.data_ptr(), xs[0], xs[1], Y.data_ptr(), ys[0], ys[1], pos.data_ptr(),
                        cos.data_ptr(), sin.data_ptr(), table[0], shape[0], shape[1], 1 if inverse else 0,
-                       _stream(stream))
+                       _raw_stream(device) if stream is None else int(stream))
     if st != DG_OK:
         raise DgError(st, "dg_rope")
     return Y
@@ -848,7 +848,8 @@ def dg_kv_append(desc, K, V, pos, cos, sin, slots, cache: KvCache, Q=None, Qout=
     rows = heads = 0
     qs = qos = (0, 0)
     if desc is not None:
-        _need(pos is not None and cos is not None and sin is not None, "a rotation takes pos, cos and sin")
+        if pos is None or cos is None or sin is None:
+            raise ValueError("a rotation takes pos, cos and sin")
         table = cos.shape
         if not (desc.dim == cache.dim and table == sin.shape and len(table) == 2 and table[1] == desc.half
                 and pos.shape == (desc.n_axes, shape[0]) and cos.dtype is _f32 and sin.dtype is _f32
@@ -858,16 +859,17 @@ def dg_kv_append(desc, K, V, pos, cos, sin, slots, cache: KvCache, Q=None, Qout=
             _check_tables(desc, pos, cos, sin, shape[0])
         d, rows, p, c, s = desc.handle, table[0], pos.data_ptr(), cos.data_ptr(), sin.data_ptr()
     if Q is not None or Qout is not None:
-        _need(Q is not None and Qout is not None and desc is not None, "Q turns into Qout by desc")
+        if Q is None or Qout is None or desc is None:
+            raise ValueError("Q turns into Qout by desc")
         qs, qos, qshape = Q.stride(), Qout.stride(), Q.shape
         if not (len(qshape) == 3 and Qout.shape == qshape and qshape[0] == shape[0] and qshape[2] == shape[2]
                 and qs[2] == 1 and qos[2] == 1 and Q.dtype is kind and Qout.dtype is kind
                 and device == Q.get_device() == Qout.get_device()):
             _check_queries(Q, Qout, shape[0], cache)
         q, qo, heads = Q.data_ptr(), Qout.data_ptr(), qshape[1]
-    st = lib().dg_kv_append(d, cache.ref, cache.in_kind, q, qs[0], qs[1], qo, qos[0], qos[1], heads, K.data_ptr(),
+    st = (_lib or lib()).dg_kv_append(d, cache.ref, cache.in_kind, q, qs[0], qs[1], qo, qos[0], qos[1], heads, K.data_ptr(),
                             ks[0], ks[1], V.data_ptr(), vs[0], vs[1], p, c, s, rows, slots.data_ptr(), shape[0],
-                            _stream(stream))
+                            _raw_stream(device) if stream is None else int(stream))
     if st != DG_OK:
         raise DgError(st, "dg_kv_append")
     return cache
@@ -927,9 +929,10 @@ def dg_attention_paged(desc: AttnDesc, Q, cache: KvCache, cu_q, kv_len, page_tab
         _need(workspace.element_size() == 1 and workspace.is_contiguous(), "workspace must be contiguous bytes")
         _here(workspace)
         ws, wb = workspace.data_ptr(), workspace.numel()
-    st = lib().dg_attention_paged(desc.handle, cache.in_kind, Q.data_ptr(), qt[0], qt[1], cache.ref, cu_q.data_ptr(),
+    st = (_lib or lib()).dg_attention_paged(desc.handle, cache.in_kind, Q.data_ptr(), qt[0], qt[1], cache.ref, cu_q.data_ptr(),
                                   kv_len.data_ptr(), page_table.data_ptr(), ts[1], tt[0], O.data_ptr(), ot[0], ot[1],
-                                  qs[0], qs[1], ts[0], max_q, max_kv, qk_scale, ws, wb, _stream(stream))
+                                  qs[0], qs[1], ts[0], max_q, max_kv, qk_scale, ws, wb,
+                                  _raw_stream(device) if stream is None else int(stream))
     if st != DG_OK:
         raise DgError(st, "dg_attention_paged")
     return O

@@ -426,6 +426,68 @@ def test_bad_pages_and_lengths(dg):
         b.cu[2] = 4
 
 
+def test_bounds_below_the_lengths(dg):
+    """New tokens past max_q are left as they are, keys past max_kv are not read."""
+    import torch
+    b = Batch(dg, [1, 3, 40], [300, 200, 260], 8, 2, 128, seed=12)
+    for split in (0, 64):
+        desc = dict(causal=1, split_keys=split, exp2="inst")
+        want = b.run(dg, desc)
+        got = b.run(dg, desc, max_q=2)
+        same(got[:3], want[:3])
+        same(got[4:6], want[4:6])
+        assert (got[3:4] == 3.0).all() and (got[6:] == 3.0).all()
+        got = b.run(dg, desc, max_kv=130)
+        cut = b.kv.clamp(max=130)
+        b.kv, keep = cut, b.kv
+        same(got, b.run(dg, desc))
+        b.kv = keep
+        assert (b.run(dg, desc, max_kv=0) == 0).all()
+
+
+def test_two_streams_and_two_threads_at_once(dg):
+    """Calls of one descriptor and cache on two streams, each with a workspace of its own, and
+    from two host threads on one stream."""
+    import threading
+
+    import torch
+    desc = dict(causal=1, split_keys=64, exp2="inst")
+    a = Batch(dg, [1] * 24, list(range(100, 2500, 100)), 8, 2, 128, seed=20)
+    b = Batch(dg, [2, 30], [1900, 700], 8, 2, 128, seed=21)
+    wanted = {x: x.run(dg, desc) for x in (a, b)}
+    torch.cuda.synchronize()
+    streams = {a: torch.cuda.Stream(), b: torch.cuda.Stream()}
+    queries = {x: x.q.cuda() for x in (a, b)}
+    torch.cuda.synchronize()
+    got = {a: [], b: []}
+    for _ in range(10):
+        for x in (a, b):
+            with torch.cuda.stream(streams[x]):
+                got[x].append(x.run(dg, desc, q=queries[x]))
+    torch.cuda.synchronize()
+    for x in (a, b):
+        for y in got[x]:
+            same(y, wanted[x])
+    one = torch.cuda.Stream()
+    got = {a: [], b: []}
+
+    def work(x):
+        with torch.cuda.stream(one):
+            for _ in range(10):
+                got[x].append(x.run(dg, desc, q=queries[x]))
+
+    threads = [threading.Thread(target=work, args=(x,)) for x in (a, b)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for x in (a, b):
+        assert len(got[x]) == 10
+        for y in got[x]:
+            same(y, wanted[x])
+
+
 def test_strides_and_streams(dg):
     """Queries inside a fused projection, outputs inside a wider row, a page table that is part
     of a wider one, on another stream than the current one."""
