@@ -141,7 +141,7 @@ struct RopeArgs {
   const int64_t* slots;          // T (append)
   int64_t T, table_rows;
   int32_t dim, half, adjacent, n_axes, inverse;
-  int32_t in_dtype, kv_dtype, append;
+  int32_t in_dtype, kv_dtype;
   int64_t page_stride, token_stride, head_stride, n_slots;   // the cache, in elements
   int32_t page_size;
   uint32_t page_mul, page_shift;   // slot / page_size, as PagedArgs

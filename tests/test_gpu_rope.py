@@ -73,6 +73,8 @@ CASES = [  # T, H, dim, rotary, pairing, axes kind, dtype
     (19, 9, 128, 64, "half", 3, "float32"), (65, 4, 64, 32, "adjacent", 2, "bfloat16"), (5, 33, 80, 80, "half", 3, "float16"),
     (4, 2, 96, 48, "half", 4, "bfloat16"), (3, 2, 36, 20, "adjacent", 2, "float32"), (130, 1, 512, 512, "half", 4, "bfloat16"),
     (11, 6, 72, 72, "half", "mixed", "bfloat16"), (9, 2, 128, 112, "adjacent", "mixed", "float16"), (1025, 32, 128, 128, "half", 3, "bfloat16"),
+    # outputs past 32 MB
+    (4200, 32, 128, 128, "half", 3, "bfloat16"), (2101, 32, 128, 96, "adjacent", 1, "float32"),
 ]
 
 
