@@ -39,181 +39,183 @@ attn_paged(PagedArgs a) {
   // The walk for the tile's rows from .. to - 1.  False, with nothing written: a
   // value that is not finite lies where only some of them see it.
   auto walk = [&](int from, int to) {
-  from = __builtin_amdgcn_readfirstlane(from);       // uniform, which the loop around hides
-  to = __builtin_amdgcn_readfirstlane(to);
-  const int end = visible(a, sq, (to - 1) / a.g);    // keys that some of the rows see
-  const int vis_first = visible(a, sq, from / a.g);  // and that all see
-  const int nb = (end + W - 1) / W;
-  const int b0 = a.rec ? span * a.span_blocks : 0;
-  const int b1 = a.rec && b0 + a.span_blocks < nb ? b0 + a.span_blocks : nb;
-  if (span > 0 && b0 >= nb) return true;
+    from = __builtin_amdgcn_readfirstlane(from);       // uniform, which the loop around hides
+    to = __builtin_amdgcn_readfirstlane(to);
+    const int end = visible(a, sq, (to - 1) / a.g);    // keys that some of the rows see
+    const int vis_first = visible(a, sq, from / a.g);  // and that all see
+    const int nb = (end + W - 1) / W;
+    const int b0 = a.rec ? span * a.span_blocks : 0;
+    const int b1 = a.rec && b0 + a.span_blocks < nb ? b0 + a.span_blocks : nb;
+    if (span > 0 && b0 >= nb) return true;
 
-  int lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));                        // (its addresses are worked out per walk: registers)
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                        // (its addresses are worked out per walk: registers)
     lane &= 63;
-  const int li = lane & (RW - 1), G = lane / RW, r = r0 + RW * wave + li;
-  const bool valid = r >= from && r < to;
-  const int tok = valid ? r / a.g : 0, head = kvh * a.g + (valid ? r % a.g : 0);
-  const int vis = valid ? visible(a, sq, tok) : end;
-  const int vis_least = __builtin_amdgcn_readfirstlane(vis);   // no row of the wave sees fewer (or none is valid)
+    const int li = lane & (RW - 1), G = lane / RW, r = r0 + RW * wave + li;
+    const bool valid = r >= from && r < to;
+    // (rows that are not there: the first one again)
+    const int rr = valid ? r : from, tok = rr / a.g, head = kvh * a.g + rr % a.g;
+    const int vis = valid ? visible(a, sq, tok) : end;
+    const int vis_least = __builtin_amdgcn_readfirstlane(vis);   // no row of the wave sees fewer (or none is valid)
 
-  const int k0 = Tile::k_place(lane), v0 = Tile::v_place(lane);
+    const int k0 = Tile::k_place(lane), v0 = Tile::v_place(lane);
 
-  shortx8 qf[QKS];
-  const uint16_t* Qr = a.Q + (int64_t)(sq.q0 + tok) * a.q_token + head * a.q_head;
+    shortx8 qf[QKS];
+    const uint16_t* Qr = a.Q + (int64_t)(sq.q0 + tok) * a.q_token + head * a.q_head;
 #pragma unroll
-  for (int k = 0; k < QKS; ++k)
-    qf[k] = *(const shortx8*)&Qr[Tile::KS * k + 8 * G];   // (rows that are not there: the first one's)
+    for (int k = 0; k < QKS; ++k)
+      qf[k] = *(const shortx8*)&Qr[Tile::KS * k + 8 * G];
 
-  Tile t;
-  t.tl = (lds_f4*)joined + (JOINS && TL ? 64 * (TL / 4) * wave + lane : 0);
-  t.start();
+    Tile t;
+    t.tl = (lds_f4*)joined + (JOINS && TL ? 64 * (TL / 4) * wave + lane : 0);
+    t.start();
 
-  // a wave loads RPW rows of a block; lane j finds row j % RPW (asked for a block
-  // before its use; lanes of one row write the same)
-  const int64_t Kb = (int64_t)a.K + (int64_t)kvh * a.head_stride, Vb = (int64_t)a.V + (int64_t)kvh * a.head_stride;
-  const int32_t* table = a.page_table + (int64_t)bat * a.table_stride;
-  const int last = end < W * b1 ? end : W * b1;        // the walk's last key, and one
-  const int own_row = RPW * wave + (lane & (RPW - 1));
-  Row row;
-  row.start(a, W * b0 + own_row);
-  auto ask = [&]() { row.ask(a, table, last); };
-  auto locate = [&](int b) {
-    where[b & 3][own_row] = row.locate(a, Kb, Vb);
-    asm volatile("" ::: "memory");               // other lanes of the wave read it
-  };
-  // straight into LDS (the lane fetches the piece that belongs at its place), or
-  // e4m3 into registers and from there, widened, into LDS
-  u32x4 kr[E8 ? NLD : 1], vr[E8 ? NLD : 1];
-  auto fetch = [&](bool v, lds_u16 dst, int b) {
-    if (b >= b1) return;
-#pragma unroll
-    for (int i = 0; i < NLD; ++i) {
-      const unsigned q = 64 * (NLD * wave + i) + lane, t = q / MC;
-      if constexpr (E8) {
-        (v ? vr : kr)[i] = *(const __attribute__((address_space(1))) u32x4*)((glb_bytes)(v ? where[b & 3][t].v : where[b & 3][t].k) + 16 * (q % MC));
-      } else {
-        const int c = (q % MC) ^ (v ? v_swz<RW, DC>(t) : k_swz<RW, DC>(t));
-        __builtin_amdgcn_global_load_lds((glb_void)((glb_bytes)(v ? where[b & 3][t].v : where[b & 3][t].k) + 16 * c),
-                                         (lds_void)(dst + 512 * (NLD * wave + i)), 16, 0, 0);
-      }
-    }
-  };
-  auto stash = [&](bool v, lds_u16 dst, int b) {
-    if constexpr (E8) {
+    // a wave loads RPW rows of a block; lane j finds row j % RPW (asked for a block
+    // before its use; lanes of one row write the same)
+    const int64_t Kb = (int64_t)a.K + (int64_t)kvh * a.head_stride, Vb = (int64_t)a.V + (int64_t)kvh * a.head_stride;
+    const int32_t* table = a.page_table + (int64_t)bat * a.table_stride;
+    const int last = end < W * b1 ? end : W * b1;        // the walk's last key, and one
+    const int own_row = RPW * wave + (lane & (RPW - 1));
+    Row row;
+    row.start(a, W * b0 + own_row);
+    auto ask = [&]() { row.ask(a, table, last); };
+    auto locate = [&](int b) {
+      where[b & 3][own_row] = row.locate(a, Kb, Vb);
+      asm volatile("" ::: "memory");               // other lanes of the wave read it
+    };
+    // straight into LDS (the lane fetches the piece that belongs at its place), or
+    // e4m3 into registers and from there, widened, into LDS
+    u32x4 kr[E8 ? NLD : 1], vr[E8 ? NLD : 1];
+    auto fetch = [&](bool v, lds_u16 dst, int b) {
       if (b >= b1) return;
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
-        const unsigned q = 64 * (NLD * wave + i) + lane, t = q / MC, c = 2 * (q % MC);
-        const int z = v ? v_swz<RW, DC>(t) : k_swz<RW, DC>(t);
-        const u32x4 x = (v ? vr : kr)[i];
+        const unsigned q = 64 * (NLD * wave + i) + lane, t = q / MC;
+        if constexpr (E8) {
+          (v ? vr : kr)[i] = *(const __attribute__((address_space(1))) u32x4*)((glb_bytes)(v ? where[b & 3][t].v : where[b & 3][t].k) + 16 * (q % MC));
+        } else {
+          const int c = (q % MC) ^ (v ? v_swz<RW, DC>(t) : k_swz<RW, DC>(t));
+          __builtin_amdgcn_global_load_lds((glb_void)((glb_bytes)(v ? where[b & 3][t].v : where[b & 3][t].k) + 16 * c),
+                                           (lds_void)(dst + 512 * (NLD * wave + i)), 16, 0, 0);
+        }
+      }
+    };
+    auto stash = [&](bool v, lds_u16 dst, int b) {
+      if constexpr (E8) {
+        if (b >= b1) return;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *(lds_x4*)&dst[8 * (t * DC + ((c + h) ^ z))] =
-              u32x4{e4m3x2_bf16x2<false>(x[2 * h]), e4m3x2_bf16x2<true>(x[2 * h]), e4m3x2_bf16x2<false>(x[2 * h + 1]),
-                    e4m3x2_bf16x2<true>(x[2 * h + 1])};
+        for (int i = 0; i < NLD; ++i) {
+          const unsigned q = 64 * (NLD * wave + i) + lane, t = q / MC, c = 2 * (q % MC);
+          const int z = v ? v_swz<RW, DC>(t) : k_swz<RW, DC>(t);
+          const u32x4 x = (v ? vr : kr)[i];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            *(lds_x4*)&dst[8 * (t * DC + ((c + h) ^ z))] =
+                u32x4{e4m3x2_bf16x2<false>(x[2 * h]), e4m3x2_bf16x2<true>(x[2 * h]), e4m3x2_bf16x2<false>(x[2 * h + 1]),
+                      e4m3x2_bf16x2<true>(x[2 * h + 1])};
+        }
+      }
+    };
+    auto load_k = [&](lds_u16 K_, int base, int u) {
+      return *(const lds_s8*)&K_[(base ^ (Tile::KS * (u % QKS))) + Tile::tile_key(u / QKS) * D];
+    };
+
+    // P~ is 0 where a row does not see a key, and so is 0 x V, but for an infinity
+    // or a NaN: looked for in the blocks with keys that only some of the rows see
+    // (a decoding step has none), and told to all waves after the next barrier.
+    // (of the blocks by parity: a wave past the barrier may look at the next one).
+    bool looked = false;
+    auto look = [&](int b, lds_u16 V_) {
+      looked = vis_first < (W * b + W < end ? W * b + W : end);
+      if (!looked) return;
+      uint32_t bad = 0;
+#pragma unroll 4
+      for (int i = 0; i < W * DC / (64 * NW); ++i)
+        bad |= not_finite<F16>(*(const lds_x4*)&V_[8 * (64 * (NW * i + wave) + lane)]);
+      if (__builtin_amdgcn_ballot_w64(bad != 0)) spoilt[b & 1] = 1;   // (by all lanes)
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    auto found = [&](int b) { return looked && __builtin_amdgcn_readfirstlane(*(volatile int*)&spoilt[b & 1]) != 0; };
+
+    // A wave's own loads have landed once its count is zero (its LDS writes once
+    // theirs is); after the barrier that follows, everybody's have, and the K
+    // pair of block b and the V pair of block b - 1 are free for the loads of
+    // blocks b + 2 and b + 1.
+    auto turn = [&]() {
+      if constexpr (E8) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+      barrier_nofence();
+    };
+    int folded = 0;                                // first block of the span being walked (a.rec null)
+    auto step = [&](int b, lds_u16 Vc, lds_u16 Vn, lds_u16 Kc, lds_u16 Kn) {
+      turn();
+      if (found(b - 1)) return false;
+      look(b, Vc);
+      if constexpr (E8) {
+        stash(false, Kc, b + 2);
+        stash(true, Vn, b + 1);
+        locate(b + 3);
+        fetch(false, Kc, b + 3);
+        fetch(true, Vn, b + 2);
+        ask();
+      } else {
+        locate(b + 2);
+        fetch(false, Kc, b + 2);
+        fetch(true, Vn, b + 1);
+        ask();
+      }
+      int k1 = k0, v1 = v0;
+      asm volatile("" : "+v"(k1), "+v"(v1));       // (their steps worked out per block: registers)
+      t.block(a, W * b, vis, vis_least, G, Vc, v1, qf, [&](int u) { return load_k(Kn, k1, u); });
+      if constexpr (JOINS) if (b + 1 - folded == a.span_blocks || b + 1 == b1) {
+        t.fold(W * folded, vis);
+        folded = b + 1;
+      }
+      return true;
+    };
+    spoilt[threadIdx.x & 1] = 0;
+    bool whole = true;
+    if (b0 < b1) {
+      ask();
+      locate(b0);
+      fetch(false, (lds_u16)K0, b0);
+      fetch(true, (lds_u16)V0, b0);
+      stash(false, (lds_u16)K0, b0);
+      stash(true, (lds_u16)V0, b0);
+      ask();
+      locate(b0 + 1);
+      if constexpr (E8) {
+        fetch(false, (lds_u16)K1, b0 + 1);
+        stash(false, (lds_u16)K1, b0 + 1);
+        fetch(true, (lds_u16)V1, b0 + 1);
+        ask();
+        locate(b0 + 2);
+        fetch(false, (lds_u16)K0, b0 + 2);
+        ask();
+        turn();
+      } else {
+        turn();
+        fetch(false, (lds_u16)K1, b0 + 1);
+        ask();
+      }
+#pragma unroll
+      for (int u = 0; u < NQ; ++u) t.score(u, load_k((lds_u16)K0, k0, u), qf[u % QKS]);
+      for (int b = b0; whole && b < b1; b += 2) {
+        whole = step(b, (lds_u16)V0, (lds_u16)V1, (lds_u16)K0, (lds_u16)K1);
+        if (whole && b + 1 < b1) whole = step(b + 1, (lds_u16)V1, (lds_u16)V0, (lds_u16)K1, (lds_u16)K0);
+      }
+      if (looked) {
+        // the last block's finding; and nobody clears it, or loads for the next
+        // walk, before all waves are here
+        turn();
+        whole = whole && !found(b1 - 1);
+        turn();
+        if (!whole) return false;
       }
     }
-  };
-  auto load_k = [&](lds_u16 K_, int base, int u) {
-    return *(const lds_s8*)&K_[(base ^ (Tile::KS * (u % QKS))) + Tile::tile_key(u / QKS) * D];
-  };
 
-  // P~ is 0 where a row does not see a key, and so is 0 x V, but for an infinity
-  // or a NaN: looked for in the blocks with keys that only some of the rows see
-  // (a decoding step has none), and told to all waves after the next barrier.
-  // (of the blocks by parity: a wave past the barrier may look at the next one).
-  bool looked = false;
-  auto look = [&](int b, lds_u16 V_) {
-    looked = vis_first < (W * b + W < end ? W * b + W : end);
-    if (!looked) return;
-    uint32_t bad = 0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < W * DC; i += 64 * NW) bad |= not_finite<F16>(*(const lds_x4*)&V_[8 * i]);
-    if (bad) spoilt[b & 1] = 1;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  };
-  auto found = [&](int b) { return looked && __builtin_amdgcn_readfirstlane(*(volatile int*)&spoilt[b & 1]) != 0; };
-
-  // A wave's own loads have landed once its count is zero (its LDS writes once
-  // theirs is); after the barrier that follows, everybody's have, and the K
-  // pair of block b and the V pair of block b - 1 are free for the loads of
-  // blocks b + 2 and b + 1.
-  auto turn = [&]() {
-    if constexpr (E8) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    else __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-    barrier_nofence();
-  };
-  int folded = 0;                                // first block of the span being walked (a.rec null)
-  auto step = [&](int b, lds_u16 Vc, lds_u16 Vn, lds_u16 Kc, lds_u16 Kn) {
-    turn();
-    if (found(b - 1)) return false;
-    look(b, Vc);
-    if constexpr (E8) {
-      stash(false, Kc, b + 2);
-      stash(true, Vn, b + 1);
-      locate(b + 3);
-      fetch(false, Kc, b + 3);
-      fetch(true, Vn, b + 2);
-      ask();
-    } else {
-      locate(b + 2);
-      fetch(false, Kc, b + 2);
-      fetch(true, Vn, b + 1);
-      ask();
-    }
-    int k1 = k0, v1 = v0;
-    asm volatile("" : "+v"(k1), "+v"(v1));       // (their steps worked out per block: registers)
-    t.block(a, W * b, vis, vis_least, G, Vc, v1, qf, [&](int u) { return load_k(Kn, k1, u); });
-    if constexpr (JOINS) if (b + 1 - folded == a.span_blocks || b + 1 == b1) {
-      t.fold(W * folded, vis);
-      folded = b + 1;
-    }
+    if (valid) leave(a, t, sq, bat, kvh, r, tok, head, vis, span, W * b0, G);
     return true;
-  };
-  if (threadIdx.x < 2) spoilt[threadIdx.x] = 0;
-  bool whole = true;
-  if (b0 < b1) {
-    ask();
-    locate(b0);
-    fetch(false, (lds_u16)K0, b0);
-    fetch(true, (lds_u16)V0, b0);
-    stash(false, (lds_u16)K0, b0);
-    stash(true, (lds_u16)V0, b0);
-    ask();
-    locate(b0 + 1);
-    if constexpr (E8) {
-      fetch(false, (lds_u16)K1, b0 + 1);
-      stash(false, (lds_u16)K1, b0 + 1);
-      fetch(true, (lds_u16)V1, b0 + 1);
-      ask();
-      locate(b0 + 2);
-      fetch(false, (lds_u16)K0, b0 + 2);
-      ask();
-      turn();
-    } else {
-      turn();
-      fetch(false, (lds_u16)K1, b0 + 1);
-      ask();
-    }
-#pragma unroll
-    for (int u = 0; u < NQ; ++u) t.score(u, load_k((lds_u16)K0, k0, u), qf[u % QKS]);
-    for (int b = b0; whole && b < b1; b += 2) {
-      whole = step(b, (lds_u16)V0, (lds_u16)V1, (lds_u16)K0, (lds_u16)K1);
-      if (whole && b + 1 < b1) whole = step(b + 1, (lds_u16)V1, (lds_u16)V0, (lds_u16)K1, (lds_u16)K0);
-    }
-    if (looked) {
-      // the last block's finding; and nobody clears it, or loads for the next
-      // walk, before all waves are here
-      turn();
-      whole = whole && !found(b1 - 1);
-      turn();
-      if (!whole) return false;
-    }
-  }
-
-  if (valid) leave(a, t, sq, bat, kvh, r, tok, head, vis, span, W * b0, G);
-  return true;
   };
 
   // rows whose tile holds such values are walked a token at a time: the rows of

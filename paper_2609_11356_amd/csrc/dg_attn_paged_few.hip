@@ -74,13 +74,14 @@ attn_paged_few(PagedArgs a) {
 
     const int r = li;
     const bool valid = r >= from && r < to;
-    const int tok = valid ? r / a.g : 0, head = kvh * a.g + (valid ? r % a.g : 0);
+    // (rows that are not there: the first one again)
+    const int rr = valid ? r : from, tok = rr / a.g, head = kvh * a.g + rr % a.g;
     const int vis = valid ? visible(a, sq, tok) : end;
     shortx8 qf[QKS];
     const uint16_t* Qr = a.Q + (int64_t)(sq.q0 + tok) * a.q_token + head * a.q_head;
 #pragma unroll
     for (int k = 0; k < QKS; ++k)
-      qf[k] = *(const shortx8*)&Qr[32 * k + 8 * G];   // (rows that are not there: the first one's)
+      qf[k] = *(const shortx8*)&Qr[32 * k + 8 * G];
 
     const int kmap = key_of_row<16>(li);
     const int v0 = Tile::v_place(lane);
@@ -144,7 +145,7 @@ attn_paged_few(PagedArgs a) {
         // keys that only some of the rows see: no infinity or NaN among their values?
         uint32_t bad = 0;
 #pragma unroll 4
-        for (int i = lane; i < W * DC; i += 64) bad |= not_finite<F16>(*(const lds_x4*)&Vc[8 * i]);
+        for (int i = 0; i < W * DC / 64; ++i) bad |= not_finite<F16>(*(const lds_x4*)&Vc[8 * (64 * i + lane)]);
         if (__builtin_amdgcn_ballot_w64(bad != 0)) return false;
       }
       int v1 = v0;
