@@ -656,7 +656,7 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
  *   beyond them is left out).
  *   A row that sees no key is +0.  Rows before cu_q[0] or from cu_q[batch] on
  *   are left as they are.  A page number outside the cache makes the rows that
- *   see its keys NaN; lengths beyond the table or the batch are cut.
+ *   see its keys NaN; offsets and lengths beyond the table or the batch are brought into it.
  *   workspace: device, at least dg_attention_paged_bytes, 16-byte aligned, not
  *   in use by another call or graph at the same time; or NULL: a library-owned
  *   workspace of the (device, stream), and under capture or without memory for

@@ -242,17 +242,17 @@ __global__ __launch_bounds__(64) void attn_paged_join(PagedArgs a) {
   const int lane = threadIdx.x, col = 64 * (blockIdx.x % (D / 64)) + lane;
   const int64_t id = blockIdx.x / (D / 64);
   const int Hq = a.Hkv * a.g;
-  int bat, tok, head;
+  int bat, head, row = 0, r = 0;
   if (a.rec_rows) {
     if (id >= (int64_t)a.B * a.Hkv * a.rec_rows) return;
-    const int r = (int)(id % a.rec_rows), bk = (int)(id / a.rec_rows);
+    r = (int)(id % a.rec_rows);
+    const int bk = (int)(id / a.rec_rows);
     bat = bk / a.Hkv;
-    tok = r / a.g;
     head = bk % a.Hkv * a.g + r % a.g;
   } else {
     if (id >= (int64_t)a.rows * Hq) return;
     head = (int)(id % Hq);
-    const int row = (int)(id / Hq);
+    row = (int)(id / Hq);
     // the last sequence that starts at or before the row
     int lo = 0, hi = a.B;
     while (hi - lo > 1) {
@@ -260,9 +260,11 @@ __global__ __launch_bounds__(64) void attn_paged_join(PagedArgs a) {
       if (a.cu_q[mid] <= row) lo = mid; else hi = mid;
     }
     bat = lo;
-    tok = row - a.cu_q[bat];
   }
+  // the walk's own first row, brought into the batch, not the offset as it was given; so tok is below
+  // rows, and tok * g in 31 bits
   const Seq sq = sequence(a, bat);
+  const int tok = a.rec_rows ? r / a.g : row - sq.q0;
   const int nrow = rows_of(a, sq);
   if (nrow <= a.row_lo || nrow > a.row_hi || tok < 0 || tok * a.g >= nrow) return;
   const int vis = visible(a, sq, tok), keys = 64 * a.span_blocks;
