@@ -269,7 +269,7 @@ __global__ __launch_bounds__(64) void attn_paged_join(PagedArgs a) {
   if (nrow <= a.row_lo || nrow > a.row_hi || tok < 0 || tok * a.g >= nrow) return;
   const int vis = visible(a, sq, tok), keys = 64 * a.span_blocks;
   if (vis <= keys) return;                       // answered by the span's own workgroup
-  const int n = (vis + keys - 1) / keys;
+  const int n = (vis - 1) / keys + 1;            // (vis + keys may pass 31 bits)
   const float2* ml = a.rec_ml + id * a.nspan;
   const float* rec = a.rec + id * a.nspan * D + col;
   float M = 0.f, L = 0.f, T = 0.f;

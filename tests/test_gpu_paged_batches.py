@@ -32,3 +32,36 @@ def test_offsets_below_the_first_row(dg, Hq, Hkv, dim, split):  # noqa: F811
     none.cu[:2] = none.cu[:2] - 7
     none.cu[1] = -3
     same(none.run(dg, desc)[:50], clean[:50])
+
+
+@pytest.mark.parametrize("Hq", [2, 20])
+def test_as_many_keys_as_there_may_be(dg, Hq):  # noqa: F811
+    """2^31 - 65536 keys: one page over and over, and at the end another that holds about half
+    of the weight.  The bound is test_gpu_attention_paged's for the keys of one span, with two
+    roundings of the sum and the output by every span on top."""
+    import torch
+    dim, page, split, n = 64, 8192, 131072, (1 << 31) - 65536
+    g = torch.Generator().manual_seed(33)
+    k = torch.randn(2, page, 1, dim, generator=g)
+    k[1] = 1.55 + 0.05 * k[1]
+    v = torch.randn(2, page, 1, dim, generator=g)
+    v[1] += 1.0
+    k, v = k.bfloat16(), v.bfloat16()
+    q = (1.0 + 0.1 * torch.randn(1, Hq, dim, generator=g)).bfloat16()
+    cache = dg.KvCache(k.cuda(), v.cuda())
+    table = torch.zeros((1, n // page), dtype=torch.int32, device="cuda")
+    table[0, -1] = 1
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")   # noqa: E731
+    desc = dg.AttnDesc(causal=1, split_keys=split, exp2="inst", out="f32")
+    got = dg.dg_attention_paged(desc, q.cuda(), cache, i32(0, 1), i32(n), table,
+                                torch.full((1, Hq, dim), 3.0, device="cuda"), scale(dim), 1, n).double().cpu()[0]
+    times = torch.tensor([n // page - 1, 1], dtype=torch.float64).repeat_interleave(page)
+    kk, vv, qq = k.view(-1, dim).double(), v.view(-1, dim).double(), q[0].double()
+    p = torch.softmax(qq @ kk.T * (scale(dim) / LOG2E) + times.log(), -1)
+    assert 0.2 < float(p[:, page:].sum(1).min()) and float(p[:, page:].sum(1).max()) < 0.8
+    S = (qq.abs() @ kk.abs().T).amax(1, keepdim=True) * scale(dim)
+    rel = (math.log(2) * 2 * S * (dim / 8 * 2.0 ** -23 + 2.0 ** -22) + (split / 8 + split / 64 + 32) * 2.0 ** -23
+           + n / split * 4 * 2.0 ** -24)
+    bound = (p @ vv.abs()) * (2.0 ** -8 + rel) * (1 + 2.0 ** -7)
+    assert not got.isnan().any()
+    assert ((got - p @ vv).abs() <= bound).all(), float(((got - p @ vv).abs() / bound).max())
