@@ -582,8 +582,8 @@ void dg_rope_desc_destroy(dg_rope_desc* d);
  *   Y's rows may not overlap each other.
  *   pos: device, n_axes x T int32;  cos_t, sin_t: device, table_rows x
  *   rotary / 2 fp32.
- * T = 0 or H = 0 is a no-op.  DG_ERR_SHAPE for negative sizes or strides or T
- * over 2^31 - 1, DG_ERR_INVALID for overlapping rows or a NULL pointer,
+ * T = 0 or H = 0 is a no-op.  DG_ERR_SHAPE for negative sizes or strides, T
+ * over 2^31 - 1 or rows that lie 2^62 bytes apart or more, DG_ERR_INVALID for overlapping rows or a NULL pointer,
  * DG_ERR_ALIGN for a pointer not aligned to its element.  One launch; rows and
  * strides of whole 16-byte pieces are faster. */
 dg_status dg_rope(const dg_rope_desc* d, int32_t dtype, const void* X, int64_t x_token, int64_t x_head,
@@ -668,7 +668,8 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
  * are (bf16, bf16, bf16), (f16, f16, f16) or (bf16, e4m3, bf16);  DG_ERR_SHAPE
  * for sizes out of range (rows * q_heads at most 2^28, batch 65535, batch * heads
  * 2^24, max_kv and table_width * page below 2^31 - 1024, q_heads a multiple of
- * the cache's heads, page_stride and (page - 1) * token_stride below 2^31 bytes),
+ * the cache's heads, page_stride and (page - 1) * token_stride below 2^31 bytes,
+ * rows within 2^62 bytes),
  * DG_ERR_ALIGN, DG_ERR_INVALID as elsewhere;  DG_ERR_SCRATCH for a
  * workspace that is too small. */
 dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void* Q, int64_t q_token, int64_t q_head,

@@ -1309,6 +1309,9 @@ namespace {
 struct Rows {
   const void* p;
   int64_t token, head, T, H, dim, size;   // size: bytes per element
+  bool reach() const {                    // offsets that 63 bits hold, with room
+    return ((__int128)(T - 1) * token + (__int128)(H - 1) * head + dim) * size < ((__int128)1 << 62);
+  }
   int64_t extent() const { return ((T - 1) * token + (H - 1) * head + dim) * size; }
   bool apart() const {                    // no two rows share an element
     const int64_t t = T > 1 ? token : INT64_MAX, h = H > 1 ? head : INT64_MAX;
@@ -1321,8 +1324,9 @@ struct Rows {
   }
 };
 
-// Strides small enough that no offset overflows.
+// Strides as such; with their counts they have to stay in reach too.
 bool stride_ok(int64_t s) { return s >= 0 && s < ((int64_t)1 << 40); }
+bool strides_ok(const Rows& r) { return stride_ok(r.token) && stride_ok(r.head) && r.reach(); }
 
 // Whether Y may be written while X is read: the very same rows, or none of them.
 bool in_place_or_apart(const Rows& X, const Rows& Y) {
@@ -1332,7 +1336,7 @@ bool in_place_or_apart(const Rows& X, const Rows& Y) {
 }
 
 dg_status check_turned(const Rows& X, const Rows& Y) {
-  if (!stride_ok(X.token) || !stride_ok(X.head) || !stride_ok(Y.token) || !stride_ok(Y.head)) return DG_ERR_SHAPE;
+  if (!strides_ok(X) || !strides_ok(Y)) return DG_ERR_SHAPE;
   if (!X.p || !Y.p) return DG_ERR_INVALID;
   if (!aligned(X.p, X.size) || !aligned(Y.p, Y.size)) return DG_ERR_ALIGN;
   if (!Y.apart() || !in_place_or_apart(X, Y)) return DG_ERR_INVALID;
@@ -1386,6 +1390,9 @@ dg_status check_cache(const dg_kv_cache* c) {
       c->heads > 65535 || c->dim > DG_ROPE_MAX_DIM || c->pages * c->page > INT32_MAX)
     return DG_ERR_SHAPE;
   if (!stride_ok(c->page_stride) || !stride_ok(c->token_stride) || !stride_ok(c->head_stride)) return DG_ERR_SHAPE;
+  if (((__int128)(c->pages - 1) * c->page_stride + (__int128)(c->page - 1) * c->token_stride +
+       (__int128)(c->heads - 1) * c->head_stride) * 2 >= ((__int128)1 << 62))
+    return DG_ERR_SHAPE;
   if (!c->K || !c->V) return DG_ERR_INVALID;
   const int64_t size = c->dtype == DG_E4M3 ? 1 : 2;
   if (!aligned(c->K, 16) || !aligned(c->V, 16) || c->page_stride * size % 16 || c->token_stride * size % 16 ||
@@ -1437,7 +1444,7 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
   const Rows k{K, k_token, k_head, T, c->heads, c->dim, 2}, v{V, v_token, v_head, T, c->heads, c->dim, 2};
   if (q_heads && (s = check_turned(q, qo)) != DG_OK) return s;
   if (r && (s = check_tables(pos, cos_t, sin_t, table_rows)) != DG_OK) return s;
-  if (!stride_ok(k_token) || !stride_ok(k_head) || !stride_ok(v_token) || !stride_ok(v_head)) return DG_ERR_SHAPE;
+  if (!strides_ok(k) || !strides_ok(v)) return DG_ERR_SHAPE;
   if (!K || !V || !slots) return DG_ERR_INVALID;
   if (!aligned(K, 2) || !aligned(V, 2) || !aligned(slots, 8)) return DG_ERR_ALIGN;
   dg::RopeArgs a;
@@ -1562,7 +1569,9 @@ dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void*
   if (q_dtype != (c->dtype == DG_F16 ? DG_F16 : DG_BF16)) return DG_ERR_UNSUPPORTED;
   if (table_width < 0 || !stride_ok(table_stride) || (batch > 1 && table_stride < table_width)) return DG_ERR_SHAPE;
   if (table_width > PAGED_SIZES / c->page) return DG_ERR_SHAPE;
-  if (!stride_ok(q_token) || !stride_ok(q_head) || !stride_ok(o_token) || !stride_ok(o_head)) return DG_ERR_SHAPE;
+  const Rows q{Q, q_token, q_head, rows, q_heads, c->dim, 2};
+  const Rows o{O, o_token, o_head, rows, q_heads, c->dim, d->p.out_dtype == DG_F32 ? 4 : 2};
+  if (!strides_ok(q) || !strides_ok(o)) return DG_ERR_SHAPE;
   // offsets within a page, and a page's, in 31 bits
   const int64_t bytes = c->dtype == DG_E4M3 ? 1 : 2;
   if (c->page_stride * bytes > INT32_MAX || (c->page > 1 && c->token_stride * bytes > INT32_MAX / (c->page - 1)))
@@ -1571,8 +1580,6 @@ dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void*
   if (d->p.exp2 == DG_EXP2_INST && !(qk_scale > 0.f)) return DG_ERR_INVALID;
   if (rows == 0 || q_heads == 0 || batch == 0) return DG_OK;
   if (!Q || !O || !cu_q || !kv_len || (!page_table && table_width > 0)) return DG_ERR_INVALID;
-  const Rows q{Q, q_token, q_head, rows, q_heads, c->dim, 2};
-  const Rows o{O, o_token, o_head, rows, q_heads, c->dim, d->p.out_dtype == DG_F32 ? 4 : 2};
   if (!q.pieces() || !o.pieces() || !aligned(cu_q, 4) || !aligned(kv_len, 4) || !aligned(page_table, 4)) return DG_ERR_ALIGN;
   if (!o.apart() || (const char*)Q == (const char*)O) return DG_ERR_INVALID;
   max_q = std::min(max_q, rows);

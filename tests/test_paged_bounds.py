@@ -1,0 +1,25 @@
+"""More of what positions and the paged cache refuse or reserve, through the C ABI,
+before anything is launched (no GPU: the addresses are never touched)."""
+import ctypes
+
+from paper_2609_11356_amd import dg
+from tests.test_paged_refusals import A, B, C, D, append, attend, cache, rope  # noqa: F401
+
+
+def test_strides_whose_offsets_pass_63_bits():
+    """Each stride below 2^40 and each count below 2^31, but not their products."""
+    r = dg.RopeDesc(64)
+    h = r.handle
+    far = 1 << 39
+    for bad in (dict(T=(1 << 31) - 1, xt=far, yt=far), dict(T=(1 << 31) - 1, xt=far), dict(T=(1 << 31) - 1, yt=far),
+                dict(dtype=0, T=1 << 25, yt=far)):
+        assert rope(h, **dict(dict(X=A, Y=B), **bad)) == dg.DG_ERR_SHAPE, bad
+    wide = cache(pages=1 << 27, page=8, page_stride=far)
+    assert append(h, wide) == dg.DG_ERR_SHAPE
+    d, c = dg.AttnDesc(causal=1, split_keys=64), cache()
+    far_append = lambda Q=None, Qout=None, q=512, qo=512, k=512, v=512: dg.lib().dg_kv_append(   # noqa: E731
+        h, ctypes.addressof(c), 1, Q, q, 64, Qout, qo, 64, 4, C, k, 64, C, v, 64, C, C, C, 10, C, 1 << 27, None)
+    for bad in (dict(Q=C, Qout=D, q=far), dict(Q=C, Qout=D, qo=far), dict(k=far), dict(v=far)):
+        assert far_append(**bad) == dg.DG_ERR_SHAPE, bad
+    for bad in (dict(qt=far, rows=1 << 24), dict(ot=far, rows=1 << 24)):
+        assert attend(d, c, **bad) == dg.DG_ERR_SHAPE, bad
