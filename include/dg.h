@@ -643,7 +643,7 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
  * is -inf, 0 is subtracted in its place.  With DG_EXP2_INST exp2 is the part's
  * v_exp_f32, a block's mn is x = RN32(max_t score_t * qk_scale) where x > RN32(m +
  * 8) and else m (so p_t is at most about 256), p_t = exp2(fma(score_t, qk_scale,
- * -mn)), and qk_scale has to be above 0.  So the
+ * -mn)), and qk_scale and RN32(qk_scale * k_scale) have to be above 0.  So the
  * bits of a row depend on its query, the keys that it sees and the
  * descriptor, not on the batch, the chunk that it came in, the pages or the
  * launch, and with split_keys 0 and DG_EXP2_LIB are dg_attention's.

@@ -1576,8 +1576,10 @@ dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void*
   const int64_t bytes = c->dtype == DG_E4M3 ? 1 : 2;
   if (c->page_stride * bytes > INT32_MAX || (c->page > 1 && c->token_stride * bytes > INT32_MAX / (c->page - 1)))
     return DG_ERR_SHAPE;
-  // the instruction's form takes the largest score times the scale as the largest product
-  if (d->p.exp2 == DG_EXP2_INST && !(qk_scale > 0.f)) return DG_ERR_INVALID;
+  // the instruction's form takes the largest score times the scale as the largest product, and -inf
+  // times it as -inf
+  const float score_scale = qk_scale * c->k_scale;
+  if (d->p.exp2 == DG_EXP2_INST && !(qk_scale > 0.f && score_scale > 0.f)) return DG_ERR_INVALID;
   if (rows == 0 || q_heads == 0 || batch == 0) return DG_OK;
   if (!Q || !O || !cu_q || !kv_len || (!page_table && table_width > 0)) return DG_ERR_INVALID;
   if (!q.pieces() || !o.pieces() || !aligned(cu_q, 4) || !aligned(kv_len, 4) || !aligned(page_table, 4)) return DG_ERR_ALIGN;
@@ -1621,7 +1623,7 @@ dg_status dg_attention_paged(const dg_attn_desc* d, int32_t q_dtype, const void*
   a.out_dtype = d->p.out_dtype;
   a.kv_dtype = c->dtype;
   a.inst = d->p.exp2 == DG_EXP2_INST;
-  a.qk_scale = qk_scale * c->k_scale;
+  a.qk_scale = score_scale;
   a.v_scale = c->v_scale;
   hipStream_t st = (hipStream_t)stream;
   PagedPlan plan = paged_plan(d, c, rows, q_heads, batch, max_q, max_kv);

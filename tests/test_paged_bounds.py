@@ -23,3 +23,13 @@ def test_strides_whose_offsets_pass_63_bits():
         assert far_append(**bad) == dg.DG_ERR_SHAPE, bad
     for bad in (dict(qt=far, rows=1 << 24), dict(ot=far, rows=1 << 24)):
         assert attend(d, c, **bad) == dg.DG_ERR_SHAPE, bad
+
+
+def test_scales_whose_product_is_not_above_zero():
+    """The part's exponential takes qk_scale * k_scale in binary32, which has to stay above 0:
+    0 times the -inf of a key that is not seen would be NaN."""
+    inst, lib = (dg.AttnDesc(causal=1, exp2=e) for e in ("inst", "lib"))
+    small = cache(dtype=3, k_scale=1e-30)
+    assert attend(inst, small, scale=1e-30, rows=0) == dg.DG_ERR_INVALID
+    assert attend(inst, small, scale=1e-3, rows=0) == dg.DG_OK
+    assert attend(lib, small, scale=1e-30, rows=0) == dg.DG_OK
