@@ -578,13 +578,14 @@ void dg_rope_desc_destroy(dg_rope_desc* d);
  * -s), which is also the gradient: dX from dY.
  *   X, Y: device, T tokens x H heads x dim of dtype (DG_F32, DG_BF16 or
  *   DG_F16), element (t, h, e) at t * token + h * head + e in elements.  Y
- *   may be X itself with the same strides; otherwise they may not overlap, and
- *   Y's rows may not overlap each other.
+ *   may be X itself with the same strides, or with the same strides lie between
+ *   X's rows (other heads of one fused tensor) without an element of them;
+ *   otherwise the two may not overlap, and Y's rows may not overlap each other.
  *   pos: device, n_axes x T int32;  cos_t, sin_t: device, table_rows x
  *   rotary / 2 fp32.
  * T = 0 or H = 0 is a no-op.  DG_ERR_SHAPE for negative sizes or strides, T
- * over 2^31 - 1 or rows that lie 2^62 bytes apart or more, DG_ERR_INVALID for overlapping rows or a NULL pointer,
- * DG_ERR_ALIGN for a pointer not aligned to its element.  One launch; rows and
+ * over 2^31 - 1 or rows that lie 2^62 bytes apart or more, DG_ERR_INVALID for
+ * overlapping rows or a NULL pointer, DG_ERR_ALIGN for a pointer not aligned to its element.  One launch; rows and
  * strides of whole 16-byte pieces are faster. */
 dg_status dg_rope(const dg_rope_desc* d, int32_t dtype, const void* X, int64_t x_token, int64_t x_head,
                   void* Y, int64_t y_token, int64_t y_head, const int32_t* pos, const float* cos_t,

@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstddef>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <map>
 #include <mutex>
@@ -1328,11 +1329,23 @@ struct Rows {
 bool stride_ok(int64_t s) { return s >= 0 && s < ((int64_t)1 << 40); }
 bool strides_ok(const Rows& r) { return stride_ok(r.token) && stride_ok(r.head) && r.reach(); }
 
-// Whether Y may be written while X is read: the very same rows, or none of them.
+// Whether Y, whose rows are apart, may be written while X is read: the very same rows, or
+// none of them.  Rows at the same strides may lie between each other, as heads of one fused
+// tensor do: two share an element where they start less than dim apart.
 bool in_place_or_apart(const Rows& X, const Rows& Y) {
-  if (X.p == Y.p) return (X.T <= 1 || X.token == Y.token) && (X.H <= 1 || X.head == Y.head);
+  const bool alike = (X.T <= 1 || X.token == Y.token) && (X.H <= 1 || X.head == Y.head);
+  if (X.p == Y.p) return alike;
   const char *x = (const char*)X.p, *y = (const char*)Y.p;
-  return x + X.extent() <= y || y + Y.extent() <= x;
+  if (x + X.extent() <= y || y + Y.extent() <= x) return true;
+  if (!alike) return false;
+  const int64_t first = (y - x) / X.size, last_t = X.T - 1, last_h = X.H - 1;
+  for (int64_t h = -last_h; h <= last_h; ++h) {
+    const int64_t at = first + h * X.head;                 // of the same token; the nearest one is t or beside it
+    const int64_t t = last_t ? -at / X.token : 0;
+    for (int64_t n = std::max(t - 1, -last_t); n <= std::min(t + 1, last_t); ++n)
+      if (std::abs(at + n * X.token) < X.dim) return false;
+  }
+  return true;
 }
 
 dg_status check_turned(const Rows& X, const Rows& Y) {

@@ -33,3 +33,16 @@ def test_scales_whose_product_is_not_above_zero():
     assert attend(inst, small, scale=1e-30, rows=0) == dg.DG_ERR_INVALID
     assert attend(inst, small, scale=1e-3, rows=0) == dg.DG_OK
     assert attend(lib, small, scale=1e-30, rows=0) == dg.DG_OK
+
+
+def test_views_of_one_tensor_that_share_elements():
+    """At the same strides rows may lie between each other, but not less than a head apart."""
+    r = dg.RopeDesc(64)
+    h = r.handle
+    for shift in (1, 63, 64, 64 * 7, 512 - 63, 512, 512 * 9 + 63):
+        for sign in (1, -1):
+            assert rope(h, X=B, Y=B + sign * 2 * shift) == dg.DG_ERR_INVALID, shift
+    # between the rows, but for one element; at other strides
+    for bad in (dict(xt=1024, yt=1024, Y=A + 2 * (512 - 63)), dict(xt=1024, yt=1024, xh=128, yh=128, Y=A + 2 * 63),
+                dict(xt=1024, yt=2048, Y=A + 2 * 512), dict(xt=1024, yt=1024, xh=64, yh=128, Y=A + 2 * 512)):
+        assert rope(h, X=A, **bad) == dg.DG_ERR_INVALID, bad
