@@ -585,8 +585,8 @@ void dg_rope_desc_destroy(dg_rope_desc* d);
  *   rotary / 2 fp32.
  * T = 0 or H = 0 is a no-op.  DG_ERR_SHAPE for negative sizes or strides, T
  * over 2^31 - 1 or rows that lie 2^62 bytes apart or more, DG_ERR_INVALID for
- * overlapping rows or a NULL pointer, DG_ERR_ALIGN for a pointer not aligned to its element.  One launch; rows and
- * strides of whole 16-byte pieces are faster. */
+ * overlapping rows or a NULL pointer, DG_ERR_ALIGN for a pointer not aligned to
+ * its element.  One launch; rows and strides of whole 16-byte pieces are faster. */
 dg_status dg_rope(const dg_rope_desc* d, int32_t dtype, const void* X, int64_t x_token, int64_t x_head,
                   void* Y, int64_t y_token, int64_t y_head, const int32_t* pos, const float* cos_t,
                   const float* sin_t, int64_t table_rows, int64_t T, int64_t H, int32_t inverse, void* stream);
@@ -619,8 +619,9 @@ typedef struct {
  *   r NULL: nothing turns (Q must be NULL; pos and the tables are not read).
  * Two tokens with one slot leave one of them there, or parts of both: give
  * every token a slot of its own.  T = 0 is a no-op.  One launch.  Errors as
- * dg_rope, DG_ERR_UNSUPPORTED for a pair of types that is not listed,
- * DG_ERR_SHAPE for a rotation of another dim than the cache's. */
+ * dg_rope, DG_ERR_INVALID too for a cache whose rows share elements (heads of
+ * stride 0, which attention reads), DG_ERR_UNSUPPORTED for a pair of types that
+ * is not listed, DG_ERR_SHAPE for a rotation of another dim than the cache's. */
 dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_dtype, const void* Q,
                        int64_t q_token, int64_t q_head, void* Qout, int64_t qo_token, int64_t qo_head,
                        int64_t q_heads, const void* K, int64_t k_token, int64_t k_head, const void* V,

@@ -1396,6 +1396,20 @@ float exact_inverse(float scale) {
   return std::frexp(scale, &e) == 0.5f && e > -100 && e < 100 ? 1.0f / scale : 0.f;
 }
 
+// Whether no two rows of the cache share an element: its three axes nested in each other, in
+// any order.
+bool cache_apart(const dg_kv_cache& c) {
+  std::pair<int64_t, int64_t> axis[3] = {{c.page_stride, c.pages}, {c.token_stride, c.page}, {c.head_stride, c.heads}};
+  std::sort(axis, axis + 3);
+  int64_t size = c.dim;
+  for (const auto& [stride, n] : axis) {
+    if (n == 1) continue;
+    if (stride < size) return false;
+    size += (n - 1) * stride;
+  }
+  return true;
+}
+
 dg_status check_cache(const dg_kv_cache* c) {
   if (!c || c->struct_size < sizeof(dg_kv_cache)) return DG_ERR_INVALID;
   if (c->dtype != DG_BF16 && c->dtype != DG_F16 && c->dtype != DG_E4M3) return DG_ERR_INVALID;
@@ -1451,6 +1465,7 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
   if (in_dtype != c->dtype && !(in_dtype == DG_BF16 && c->dtype == DG_E4M3)) return DG_ERR_UNSUPPORTED;
   if (!Q != !Qout || (Q && !r) || c->K == c->V) return DG_ERR_INVALID;
   if (T < 0 || T > INT32_MAX || q_heads < 0 || q_heads > 65535 || (r && r->p.dim != c->dim) || c->dim % 2) return DG_ERR_SHAPE;
+  if (!cache_apart(*c)) return DG_ERR_INVALID;
   if (T == 0) return DG_OK;
   if (!Q) q_heads = 0;
   const Rows q{Q, q_token, q_head, T, q_heads, c->dim, 2}, qo{Qout, qo_token, qo_head, T, q_heads, c->dim, 2};

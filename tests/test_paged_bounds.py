@@ -46,3 +46,18 @@ def test_views_of_one_tensor_that_share_elements():
     for bad in (dict(xt=1024, yt=1024, Y=A + 2 * (512 - 63)), dict(xt=1024, yt=1024, xh=128, yh=128, Y=A + 2 * 63),
                 dict(xt=1024, yt=2048, Y=A + 2 * 512), dict(xt=1024, yt=1024, xh=64, yh=128, Y=A + 2 * 512)):
         assert rope(h, X=A, **bad) == dg.DG_ERR_INVALID, bad
+
+
+def test_append_to_rows_that_share_memory():
+    """Attention reads a cache whose heads or pages are one and the same; an append would leave
+    there what came last."""
+    r, d = dg.RopeDesc(64), dg.AttnDesc(causal=1)
+    h = r.handle
+    for shared in (dict(head_stride=0), dict(token_stride=0), dict(page_stride=0), dict(head_stride=32),
+                   dict(token_stride=64, head_stride=64), dict(page_stride=1920), dict(page_stride=64, token_stride=640)):
+        assert append(h, cache(**shared)) == dg.DG_ERR_INVALID, shared
+        assert attend(d, cache(**shared), rows=0) == dg.DG_OK, shared
+    # of one head, token or page the stride does not count; any order of the three
+    for fine in (dict(heads=1, head_stride=0), dict(pages=1, page_stride=0), dict(page=1, token_stride=0),
+                 dict(token_stride=64, head_stride=1024), dict(page_stride=128, token_stride=1280)):
+        assert append(h, cache(**fine), T=0) == dg.DG_OK, fine
