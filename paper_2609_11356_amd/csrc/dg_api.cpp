@@ -1531,9 +1531,11 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
   const int64_t g = q_heads / c->heads, most = max_q * g, split = d->p.split_keys;
   p.nspan = split ? (int32_t)std::max<int64_t>(1, (max_kv + split - 1) / split) : 1;
   const bool spans = p.nspan > 1 && p.nspan <= 65535 && p.nspan * batch * c->heads <= PAGED_WORKGROUPS;
-  if (most <= 16 || batch > 1) {
+  // whole tokens of at most 16 rows (none: groups of more than 16 heads, whose tokens all are longer)
+  const int64_t few = std::min(most, 16 / g * g);
+  if (few > 0 && (most <= 16 || batch > 1)) {
     PagedLaunch& l = p.l[p.n++];
-    l = PagedLaunch{1, 16, 0, 16, (int32_t)std::min<int64_t>(most, 16), spans, 0};
+    l = PagedLaunch{1, 16, 0, 16, (int32_t)few, spans, 0};
     l.records = (size_t)batch * c->heads * l.rec_rows;
   }
   if (most > 16) {

@@ -65,3 +65,20 @@ def test_as_many_keys_as_there_may_be(dg, Hq):  # noqa: F811
     bound = (p @ vv.abs()) * (2.0 ** -8 + rel) * (1 + 2.0 ** -7)
     assert not got.isnan().any()
     assert ((got - p @ vv).abs() <= bound).all(), float(((got - p @ vv).abs() / bound).max())
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(32, 1), (17, 1), (3, 1), (15, 3)])
+def test_groups_that_16_rows_do_not_hold_whole(dg, Hq, Hkv):  # noqa: F811
+    """Single tokens, drafted ones and a chunk of heads in groups of 32, 17, 3 and 5."""
+    q = [1, 5, 1, 40, 3, 16]
+    b = Batch(dg, q, [200, 333, 1, 500, 64, 129], Hq, Hkv, 64, seed=34)
+    desc = dict(causal=1, split_keys=64, exp2="inst")
+    want = b.run(dg, desc)
+    check(b, want, desc)
+    same(b.run(dg, desc, workspace=b.space(dg, desc)), want)
+    same(captured(b, dg, desc), want)
+    at = 0
+    for i, n in enumerate(q):
+        one = Batch(dg, [n], [b.kv_lens[i]], Hq, Hkv, 64, dense=([b.dense[i]], b.q[at:at + n]))
+        same(one.run(dg, desc), want[at:at + n])
+        at += n

@@ -61,3 +61,18 @@ def test_append_to_rows_that_share_memory():
     for fine in (dict(heads=1, head_stride=0), dict(pages=1, page_stride=0), dict(page=1, token_stride=0),
                  dict(token_stride=64, head_stride=1024), dict(page_stride=128, token_stride=1280)):
         assert append(h, cache(**fine), T=0) == dg.DG_OK, fine
+
+
+def space(d, c, rows, q_heads, batch, max_q, max_kv):
+    return dg.lib().dg_attention_paged_bytes(d.handle, ctypes.addressof(c), rows, q_heads, batch, max_q, max_kv)
+
+
+def test_records_are_of_rows_that_there_may_be():
+    d, each = dg.AttnDesc(causal=1, split_keys=512), (64 + 2) * 4 * 8      # 8 spans
+    one = cache(heads=1)
+    # 32 query heads over 1: no sequence has 1 to 16 rows
+    assert space(d, one, 64, 32, 64, 1, 4096) == 64 * 32 * each
+    # 3 over 1, up to 3 tokens: 9 rows each
+    assert space(d, one, 64, 3, 64, 3, 4096) == 64 * 9 * each
+    # tokens one at a time: no row too many
+    assert space(d, cache(heads=8, page_stride=8192, token_stride=512), 64, 32, 64, 1, 4096) == 64 * 32 * each
