@@ -82,3 +82,84 @@ def test_groups_that_16_rows_do_not_hold_whole(dg, Hq, Hkv):  # noqa: F811
         one = Batch(dg, [n], [b.kv_lens[i]], Hq, Hkv, 64, dense=([b.dense[i]], b.q[at:at + n]))
         same(one.run(dg, desc), want[at:at + n])
         at += n
+
+
+@pytest.mark.parametrize("dim,Hq,Hkv,dtype,cache", [(64, 8, 8, "bfloat16", None), (64, 16, 8, "float16", None),
+                                                    (128, 16, 8, "bfloat16", None), (128, 8, 8, "bfloat16", "float8_e4m3fn"),
+                                                    (64, 12, 12, "bfloat16", "float8_e4m3fn")])
+def test_neighbouring_heads_on_one_xcd(dg, dim, Hq, Hkv, dtype, cache):  # noqa: F811
+    """Spans x sequences x key heads for some rounds of the chip: the heads of a span share an
+    XCD and the spans' order turns from sequence to sequence."""
+    lens = [1 + (149 * i) % 1100 for i in range(38)] + [1152]
+    b = Batch(dg, [1 + i % 2 for i in range(39)], [n + 1 for n in lens], Hq, Hkv, dim, dtype, cache, page=32, seed=37,
+              k_scale=0.0625 if cache else 1.0, v_scale=0.021 if cache else 1.0)
+    p = "f16" if dtype == "float16" else "bf16"
+    desc = dict(causal=1, split_keys=64, exp2="inst", p_dtype=p, out=p)
+    assert -(-b.max_kv // 64) * 39 * Hkv >= 4096
+    got = b.run(dg, desc)
+    check(b, got, desc)
+    same(got, captured(b, dg, desc))
+    same(got, captured(b, dg, desc, replays=3, workspace=b.space(dg, desc)))
+
+
+@pytest.mark.parametrize("exp2", ["inst", "lib"])
+@pytest.mark.parametrize("kv", [[1024, 1025], [1088, 2112, 2560], [2049, 64, 65, 1]])
+def test_more_spans_than_a_join_fetches_at_once(dg, kv, exp2):  # noqa: F811
+    """16, 17, 33 and 40 spans, of few rows and of a chunk."""
+    for q in ([1] * len(kv), [1] * (len(kv) - 2) + [24, 1]):
+        b = Batch(dg, q, kv, 4, 2, 128, seed=39)
+        desc = dict(causal=1, split_keys=64, exp2=exp2)
+        got = b.run(dg, desc)
+        check(b, got, desc)
+        same(got, captured(b, dg, desc))
+
+
+def test_two_streams_against_64_bits(dg):  # noqa: F811
+    import torch
+    desc = dict(causal=1, split_keys=64, exp2="inst")
+    a = Batch(dg, [1] * 24, list(range(100, 2500, 100)), 8, 2, 128, seed=41)
+    b = Batch(dg, [2, 30], [1900, 700], 8, 2, 128, seed=42)
+    queries = {x: x.q.cuda() for x in (a, b)}
+    streams = {a: torch.cuda.Stream(), b: torch.cuda.Stream()}
+    torch.cuda.synchronize()
+    got = {a: [], b: []}
+    for _ in range(4):
+        for x in (a, b):
+            with torch.cuda.stream(streams[x]):
+                got[x].append(x.run(dg, desc, q=queries[x]))
+    torch.cuda.synchronize()
+    for x in (a, b):
+        check(x, got[x][0], desc)
+        for y in got[x]:
+            same(y, got[x][0])
+
+
+@pytest.mark.parametrize("exp2,split", [("inst", 64), ("lib", 64), ("inst", 0)])
+@pytest.mark.parametrize("g", [1, 3, 5])
+@pytest.mark.parametrize("dtype,cache", [("bfloat16", None), ("float16", None), ("bfloat16", "float8_e4m3fn")])
+def test_unseen_values_in_every_type(dg, dtype, cache, g, exp2, split):  # noqa: F811
+    """NaN, infinite and the largest values reach the tokens that see them alone, in tiles whose
+    rows are not whole tokens too, with records and with one workgroup for all of a row's spans."""
+    import torch
+    p = "f16" if dtype == "float16" else "bf16"
+    desc = dict(causal=1, split_keys=split, exp2=exp2, p_dtype=p, out=p)
+    for n, m, dim, at in ((3, 200, 64, 199), (4, 130, 128, 127), (150, 300, 128, 210), (70, 200, 64, 131)):
+        base = Batch(dg, [n], [m], 2 * g, 2, dim, dtype, cache, seed=43 + n)
+        clean = base.run(dg, desc)
+        first = at - (m - n)                        # the first token that sees key `at`
+        for bad in [math.nan, torch.finfo(base.dense[0].dtype).max] + ([] if cache else [math.inf]):
+            dense = base.dense[0].clone()
+            if cache:
+                dense.view(torch.uint8)[at, 1, 0, 5] = 0x7f if math.isnan(bad) else 0x7e
+            else:
+                dense[at, 1, 0, 5] = bad
+            b = Batch(dg, [n], [m], 2 * g, 2, dim, dtype, cache, dense=([dense], base.q))
+            for got in (b.run(dg, desc), captured(b, dg, desc)):
+                same(got[:first], clean[:first])
+                same(got[:, g:], clean[:, g:])
+                same(got[..., :5], clean[..., :5])
+                same(got[..., 6:], clean[..., 6:])
+                if math.isnan(bad):
+                    assert got[first:, :g, 5].isnan().all()
+                elif math.isinf(bad):
+                    assert not got[first:, :g, 5].isfinite().any()
