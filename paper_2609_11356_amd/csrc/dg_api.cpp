@@ -1549,8 +1549,13 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
     if (most <= 64) l.split = spans && groups(64) < 512;
     else {
       l.rw = 32;
+      // eight waves with spans to join: not over e4m3, whose rows on their way leave no registers
+      // for them.  There four waves of 16 rows, two workgroups a CU, are 5 to 25 % faster than four
+      // of 32 (4096 tokens over 8000 keys, 32 heads over 8, spans of 512: 642 and 690 us, of 128: 718
+      // and 859; 12 sequences of 300 over 400 to 8000: 444 and 510)
+      const bool eight = p.nspan == 1 || c->dtype != DG_E4M3;
       if (c->dim == 64) l.split = spans && groups(128) < 400;
-      else if (groups(256) >= 200) l.nw = 8;
+      else if (eight && groups(256) >= 200) l.nw = 8;
       else if (groups(64) >= 400) l.rw = 16;   // (two workgroups a CU: 1023 tokens, 32 over 8 heads, 129 us, of 32 rows 151)
       else l.split = spans && groups(128) < 200;
     }

@@ -163,3 +163,24 @@ def test_unseen_values_in_every_type(dg, dtype, cache, g, exp2, split):  # noqa:
                     assert got[first:, :g, 5].isnan().all()
                 elif math.isinf(bad):
                     assert not got[first:, :g, 5].isfinite().any()
+
+
+@pytest.mark.parametrize("exp2", ["inst", "lib"])
+@pytest.mark.parametrize("split", [0, 128])
+@pytest.mark.parametrize("q,kv", [([1700], [1800]), ([300, 1, 700, 850], [400, 1000, 900, 850])])
+def test_large_chunks_over_e4m3(dg, q, kv, split, exp2):  # noqa: F811
+    """Chunks that fill the chip in 256-row tiles, over a cache of 8 bits: against 64 bits, one
+    workgroup for all of a row's spans, and single tokens."""
+    b = Batch(dg, q, kv, 32, 8, 128, "bfloat16", "float8_e4m3fn", page=64, seed=45, k_scale=0.0625, v_scale=0.021, behind=1)
+    desc = dict(causal=1, split_keys=split, exp2=exp2)
+    got = b.run(dg, desc)
+    check(b, got, desc)
+    same(got, captured(b, dg, desc))
+    at = 0
+    for i, (n, m) in enumerate(zip(q, kv)):
+        for j in (0, n // 2, n - 1):
+            end = m - n + j + 1
+            one = Batch(dg, [1], [end], 32, 8, 128, "bfloat16", "float8_e4m3fn", k_scale=0.0625, v_scale=0.021,
+                        dense=([b.dense[i][:end]], b.q[at + j:at + j + 1]))
+            same(one.run(dg, desc), got[at + j:at + j + 1])
+        at += n
