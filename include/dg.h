@@ -508,7 +508,8 @@ typedef struct {
   int32_t causal;         /* 0: no mask; 1: causal (Lq = Lk) */
   int32_t q_block;        /* BLOCK_M, >= 1: where the masked stage starts (causal) */
   int32_t block_sum;      /* DG_SEQ or DG_TREE: the row sum of a block's probabilities */
-  int32_t p_dtype;        /* DG_BF16: the type the probabilities are narrowed to */
+  int32_t p_dtype;        /* DG_BF16 (DG_F16 over a binary16 paged cache): the type the
+                             probabilities are narrowed to */
   int32_t pv_fma;         /* 1: the rescaled output row is the P.V accumulator */
   int32_t l_fma;          /* 1: the denominator update is one fused multiply-add */
   int32_t final_div;      /* DG_ATTN_DIV: O / l;  DG_ATTN_RECIP: O * (1 / l) */
@@ -524,8 +525,9 @@ typedef struct dg_attn_desc dg_attn_desc; /* opaque, immutable */
 /* Validate p and build an attention descriptor (free with
  * dg_attn_desc_destroy).  DG_ERR_INVALID for NULL arguments, a small
  * struct_size or a field out of range; DG_ERR_UNSUPPORTED for an order this
- * build cannot run: key_block other than 32, 64 or 128, p_dtype other than
- * bf16, or a causal q_block that is not a multiple of 16. */
+ * build cannot run: key_block other than 32, 64 or 128, p_dtype DG_F32, a
+ * causal q_block that is not a multiple of 16, or split_keys that is not a
+ * multiple of key_block. */
 dg_status dg_attn_desc_create(const dg_attn_params* p, dg_attn_desc** out);
 void dg_attn_desc_destroy(dg_attn_desc* d);
 
@@ -535,7 +537,8 @@ void dg_attn_desc_destroy(dg_attn_desc* d);
  *   aligned.  d is 64 or 128.  qk_scale multiplies each score (fold log2 e
  *   and 1 / sqrt(d) into it).
  * H = 0 or Lq = 0 is a no-op.  DG_ERR_SHAPE for Lk < 1, H > 65535,
- * Lq > 16 * 65535, or a causal descriptor with Lq != Lk; DG_ERR_UNSUPPORTED for another d;
+ * Lq > 16 * 65535, or a causal descriptor with Lq != Lk; DG_ERR_UNSUPPORTED for another d
+ * or for what only dg_attention_paged has (split_keys, DG_EXP2_INST, DG_F16);
  * DG_ERR_ALIGN for a pointer not 16-byte aligned.  One launch on stream; for
  * few query rows over many keys three launches through a library-owned
  * workspace of the (device, stream), attention's own (at most 320 MB; never
@@ -648,7 +651,9 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
  * -mn)), and qk_scale and RN32(qk_scale * k_scale) have to be above 0.  So the
  * bits of a row depend on its query, the keys that it sees and the
  * descriptor, not on the batch, the chunk that it came in, the pages or the
- * launch, and with split_keys 0 and DG_EXP2_LIB are dg_attention's.
+ * launch, and with split_keys 0 and DG_EXP2_LIB are dg_attention's (of scores
+ * beside which -1e6 vanishes).  Binary16 probabilities below 2^-14 are off by up
+ * to 2^-25 each, which the denominator is not.
  *   Q: device, rows x q_heads x dim of q_dtype, strides in elements of whole
  *   16-byte pieces;  O: the same rows of the descriptor's out_dtype (written,
  *   never read; may not overlap the inputs, nor its rows each other).
@@ -662,7 +667,10 @@ dg_status dg_kv_append(const dg_rope_desc* r, const dg_kv_cache* c, int32_t in_d
  *   workspace: device, at least dg_attention_paged_bytes, 16-byte aligned, not
  *   in use by another call or graph at the same time; or NULL: a library-owned
  *   workspace of the (device, stream), and under capture or without memory for
- *   it none, with one workgroup for all the spans of a row (the same bits).
+ *   it none, with one workgroup for all the spans of a row: the same bits, and the
+ *   time of one workgroup's walk over the longest context where there are few (8
+ *   single tokens of 32 heads over 8 x 128, 8000 to 16000 keys: 340 us instead of
+ *   94).  States of more than 1 GiB take none either.
  * rows, batch or q_heads of 0 is a no-op.  One launch, two for a batch of one
  * token and longer sequences, and one more to join spans.
  * DG_ERR_UNSUPPORTED unless key_block is 64, block_sum DG_TREE, pv_fma 1,

@@ -1506,7 +1506,12 @@ namespace {
 constexpr int64_t PAGED_SIZES = INT32_MAX - 1024;         // keys: 31-bit counts with room
 constexpr int64_t PAGED_ROWS = (int64_t)1 << 28;          // rows * heads: threads of a grid in 32 bits
 constexpr int64_t PAGED_WORKGROUPS = (int64_t)1 << 24;    // batch * key heads (and spans), for the same
-constexpr size_t PAGED_WORKSPACE = (size_t)1 << 30;       // more records than this: one walk per row
+// More bytes of records than this: one walk per row.  The walk is level or the faster one while
+// the contexts are well below max_kv, which the records are reserved for, and takes 1.1 to 1.8 times as
+// long where they are not.  (Against records of some sequences at a time: 256 single tokens over
+// 500 to 4000 keys, max_kv 131072, 454 us and 593, over 1000 to 64000 6980 and 6130; 15 and a chunk of
+// 500, max_kv 2^20, over 500 to 4000 163 and 293, over 1000 to 64000 1900 and 1040.)
+constexpr size_t PAGED_WORKSPACE = (size_t)1 << 30;
 
 // How a paged call is run (speed only): up to two launches, for sequences of
 // few rows and for the others, each with its spans apart (records) or walked
@@ -1544,8 +1549,10 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
     const auto groups = [&](int64_t r) {   // workgroups of r rows
       return std::min((rows * g + r - 1) / r + batch / 2, (most + r - 1) / r * batch) * c->heads;
     };
-    // few rows: 16 to a wave.  One workgroup for all the spans of a tile where
-    // the tiles fill the chip, or nearly; else the spans apart.
+    // few rows: 16 to a wave.  One workgroup for all the spans of a tile where the
+    // tiles fill the chip, or nearly; else the spans apart.  (8 tokens each of 64 sequences over
+    // 4000 to 8000 keys, 32 heads over 8, 512 workgroups: d 64 188 us and 226 apart, d 128 322
+    // and 396; of 32: 133 and 112, 200 and 201; of 4: 121 and 23, 170 and 31.)
     if (most <= 64) l.split = spans && groups(64) < 512;
     else {
       l.rw = 32;
@@ -1554,9 +1561,15 @@ PagedPlan paged_plan(const dg_attn_desc* d, const dg_kv_cache* c, int64_t rows, 
       // of 32 (4096 tokens over 8000 keys, 32 heads over 8, spans of 512: 642 and 690 us, of 128: 718
       // and 859; 12 sequences of 300 over 400 to 8000: 444 and 510)
       const bool eight = p.nspan == 1 || c->dtype != DG_E4M3;
+      // d 64, 128 rows: one chunk of 512 tokens over 8512 keys, 128 workgroups, 145 us and 87 apart, of
+      // 1500 over 9500, 375, 209 and 239, of 2048 over 10048, 512, 233 and 364; but 12 sequences of
+      // 100 over 500 to 8000, 352, 181 and 134, and 4 of 256 over 2000 to 16000, 256, 264 and 207
       if (c->dim == 64) l.split = spans && groups(128) < 400;
+      // d 128, 256 rows at once, 64, or 128 with the spans apart: 700 tokens over 8700 keys 274, 215 and
+      // 190 us, 1023 over 9023 287, 227 and 298, 1400 of 1400 55, 39 and 71, over 9400 302, 378 and 403,
+      // 2048 over 10048 355, 461 and 627; 8 sequences of 180 over 400 to 16000 -, 608 and 577
       else if (eight && groups(256) >= 200) l.nw = 8;
-      else if (groups(64) >= 400) l.rw = 16;   // (two workgroups a CU: 1023 tokens, 32 over 8 heads, 129 us, of 32 rows 151)
+      else if (groups(64) >= 400) l.rw = 16;   // (two workgroups a CU)
       else l.split = spans && groups(128) < 200;
     }
     l.records = (size_t)rows * q_heads;

@@ -196,7 +196,10 @@ namespace {
 // us, 2 497, 4 478, 8 437), or 512 bytes of larger ones (64 of 200 to 8000, 256 bytes: 1
 // head 218 us, 2 or more 209; 4 of 60000 to 131072: 281, 282 and, by 4, 287).  Less
 // work takes the XCDs in turn, which loads them more evenly (32 sequences of 300 to
-// 4500 keys: 17 us, near by 20).
+// 4500 keys: 17 us, near by 20).  From 4096 workgroups on near is the faster one for every
+// type and size (128-byte e4m3, 8 heads of 500 to 8000 keys: 32 sequences 71 us, near 64, 128
+// 274 and 228; 256-byte bf16 130 and 126, 465 and 439); at 2048 it is either (bf16 of 128
+// bytes 38.3 and 39.7, e4m3 48.0 and 39.2).
 int near_heads(const PagedArgs& a, int64_t spans) {
   const int64_t piece = a.dim * (a.kv_dtype == DG_E4M3 ? 1 : 2), most = piece <= 128 ? 1024 : 512;
   int n = 1;

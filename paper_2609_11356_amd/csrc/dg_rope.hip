@@ -9,9 +9,11 @@
 //
 // Bound: HBM.  A thread takes a unit of 2 PV elements of a head, PV pairs
 // (16-byte loads and stores), for up to HPT heads, so that the cosines and
-// sines of a unit are fetched once for all of them (two: 16384 tokens x 32 heads x
-// 128, 268 MB, 54 us; four take 134 registers, three waves a SIMD instead of four,
-// and 8192 tokens into an e4m3 cache 55 us instead of 41).
+// sines of a unit are fetched once for all of them.  Two heads: 16384 tokens x 32 x
+// 128, 268 MB, 55 us, the rate of a copy; appending 8192 tokens of 32 + 8 heads to an
+// e4m3 cache, 189 MB, 51 us (40 while the inputs are in the last-level cache; a
+// copy of as many bytes 37; nothing is moved twice: 84 MB are counted as written, 100 as
+// read).  Four heads take 134 registers, three waves a SIMD instead of four: 54 and 63 us.
 #include <algorithm>
 
 #include "dg_device.h"
@@ -229,9 +231,12 @@ hipError_t launch_heads(const RopeArgs& a, hipStream_t st) {
 }
 
 
-// An output larger than the L2s is stored past them: nothing of it would be left there for
-// its reader (16384 tokens x 32 heads x 128 bf16 65 -> 55 us, 4.9 TB/s; with the loads past
-// them too 64).
+// An output larger than the L2s is stored past them: they keep the inputs instead.
+// Inputs from memory, 16384 tokens x 32 heads x 128 bf16: 66 -> 55 us, 5.0 TB/s (with the
+// loads past them too 64); the e4m3 append of 8192 tokens 54 -> 51.  Its reader finds less
+// of it in the caches, which about evens out: with a product of the whole output behind it 51 -> 49
+// us at 32 MB, 71 -> 70 at 64, 95 -> 99 at 96, 124 -> 121 at 128, 225 -> 222 at 256; with a
+// copy 30 -> 27, 50 -> 50, 74 -> 76, 99 -> 106 and 215 -> 210.
 bool past_caches(const RopeArgs& a) {
   return a.T * a.q.heads * a.dim * (a.in_dtype == DG_F32 ? 4 : 2) >= ((int64_t)32 << 20);
 }
